@@ -277,6 +277,82 @@ int calvo_prefill_attn_batch(calvo_ctx* ctx, calvo_batch* batch, int layer, cons
 int calvo_prefill_attn_noalloc(calvo_ctx* ctx, int layer, const void* q, const void* k_suffix, const void* v_suffix,
                                void* out, const calvo_request* reqs, int n_reqs, const int32_t* cu_suffix, float scale);
 
+/* ---- A bounded cache: attention that looks back over a window, the weight that every cached token gathers from it, and eviction of
+ * the tokens that gather least.  Same pool, block tables, element types and compute stream as calvo_prefill_attn; all of it is queued behind
+ * the layer's most recent load.
+ *
+ * A request of a window batch: n_cached tokens whose K and V are in the pool (any number, also one that ends inside a block), and
+ * n_new tokens behind them that are computed now - a chunk of a prompt, or the one token of a decoding step.  Token i of the new ones is
+ * at position n_cached + i.  Position p sees position t if t <= p and (t > p - window or t < n_first). */
+typedef struct {
+  const int32_t* block_table; /* HOST: ceil((n_cached + n_new) / B) slot ids in [0, pool_blocks), pairwise distinct; read during
+                                 the call only.  A slot that takes new tokens is in no other request's table of the batch */
+  int32_t n_cached;           /* >= 0 */
+  int32_t n_new;              /* >= 0 */
+  int32_t mass_row;           /* row of the request in the arrays of calvo_attn_mass */
+  int32_t reserved;           /* 0 */
+} calvo_window_request;
+
+/* Checks, plans and describes a batch to the device once, for all layers of a step (the upload is queued on the compute stream).
+ * window >= 1 (INT32_MAX hides nothing), n_first >= 0.  Descriptors and the partial results of cut tiles are in a buffer of the plan's own,
+ * so that launches and captured graphs of different plans do not meet; those of one plan must not run at the same time.
+ * calvo_window_destroy does not wait: the buffer is used again behind the launches that were queued.  A plan whose
+ * calls were captured must outlive the graph's last replay.  It must precede calvo_destroy of its context.
+ * Errors (nothing queued): CALVO_EINVAL for NULL pointers, negative counts, window < 1, slot ids outside the pool, repeated inside a request, or
+ * that take new tokens and are in another request's table, more than 2^31 - 65537 tokens in a request, on a stream that is being captured;
+ * CALVO_ENOMEM if a request needs more slots than the pool has or a buffer cannot be had. */
+typedef struct calvo_window calvo_window;
+int calvo_window_prepare(calvo_ctx* ctx, const calvo_window_request* reqs, int n_reqs, int32_t window, int32_t n_first, calvo_window** out);
+int calvo_window_destroy(calvo_window* w);
+
+/* One layer of the batch: 1. if k_new / v_new are given, the new tokens' K and V are written to their slots (NULL: they are there);
+ * 2. out[i][h][:] = sum_t softmax_t(scale * <q[i][h], K[t][g]>) V[t][g] over the positions t that the row sees, g = h / (Hq/Hkv);
+ * 3. if lse is given, lse[i][h] = ln sum_t exp(scale * <q[i][h], K[t][g]>) over the same positions.
+ * q, out: DEVICE [new tokens of the batch][Hq][D], requests one after the other, 16-byte aligned; k_new, v_new: DEVICE [new tokens][Hkv][D];
+ * lse: DEVICE fp32 [new tokens][Hq] or NULL.  Element type, accumulation, rounding and scale as calvo_prefill_attn.  K and V of
+ * positions that a row does not see never reach its results, whatever they hold; nor does what lies behind a request's last
+ * token in its last slot.  Can be captured into a graph (k_new and v_new included): a captured call cannot wait for a load and gets
+ * CALVO_ENOTREADY while one is under way.  Errors (nothing queued): CALVO_EINVAL for a bad layer, NULL or misaligned pointers, out, lse or the
+ * layer's pool overlapping each other or an input. */
+int calvo_window_attn(calvo_window* w, int layer, const void* q, const void* k_new, const void* v_new, void* out, float* lse, float scale);
+
+/* The weight that every token of a request has gathered, per KV head: with R = the request's mass_row,
+ *     mass_out[R][g][t] = (t < n_cached ? mass_in[R][g][t] : 0) + sum over the counted rows i that see t and the query heads h of g of
+ *                         exp(scale * <q[i][h], K[t][g]> - lse[i][h]),      t = 0 .. n_cached + n_new - 1
+ * for the batch, window and first tokens of the plan; q and lse are those of the layer's calvo_window_attn (which comes before it: K of
+ * the new tokens is read from the pool).  last_rows > 0 counts only the last last_rows new tokens of every request, 0 all.  mass_in, mass_out:
+ * DEVICE fp32 [mass_rows][Hkv][mass_stride]; mass_in may be mass_out (the sums are added in place) or NULL (zeros).  Nothing else
+ * of mass_out is written.  Each sum is made in one fixed order: the same call gives the same bits.  Can be captured, as calvo_window_attn.
+ * Errors (nothing queued): CALVO_EINVAL for a bad layer, NULL or misaligned pointers, mass_stride below a request's tokens, a mass_row outside
+ * [0, mass_rows) or shared by two requests that have tokens, mass_out overlapping anything but a mass_in that is equal to it. */
+int calvo_attn_mass(calvo_window* w, int layer, const void* q, const float* lse, const float* mass_in, float* mass_out, int32_t mass_rows,
+                    int64_t mass_stride, int32_t last_rows, float scale);
+
+/* One request of an eviction: of n_tokens cached tokens, the first n_first and the last n_last stay, and of the others the n_keep - n_first -
+ * n_last that have gathered most weight, ties to the lower position (a NaN is below every number).  Every layer and KV head chooses for
+ * itself; positions are only storage here, K is moved as it is. */
+typedef struct {
+  const int32_t* src_table;   /* HOST: ceil(n_tokens / B) slots, pairwise distinct */
+  const int32_t* dst_table;   /* HOST: ceil(n_keep / B) slots, in no other table of the call */
+  int32_t n_tokens, n_keep;   /* 0 <= n_keep <= n_tokens */
+  int32_t n_first, n_last;    /* n_first + n_last <= n_keep */
+  int32_t mass_row;           /* row of the request in mass and mass_out; two requests that keep tokens have different ones */
+  int32_t reserved;           /* 0 */
+} calvo_evict_request;
+
+/* Layers [layer_begin, layer_end): for request r, KV head g and j < n_keep
+ *     kept[layer - layer_begin][r][g][j] = the position that is j-th of those that stay, ascending
+ *     K and V of token j in dst_table    = K and V of token kept[..][j] in src_table
+ *     mass_out[layer - layer_begin][mass_row][g][j] = mass[layer - layer_begin][mass_row][g][kept[..][j]]     (unless mass_out is NULL)
+ * mass: DEVICE fp32 [layers][mass_rows][Hkv][mass_stride]; mass_out the same with out_stride; kept: DEVICE int32
+ * [layers][n_reqs][Hkv][kept_stride].  Nothing else is written.  With dst_table the request goes on as one of n_keep cached tokens, and the source
+ * slots can be given back (calvo_pool_release) once the compute stream has passed the call: loads run on streams of their own.
+ * Queued on the compute stream; returns at once; cannot be captured.  Errors (nothing queued): CALVO_EINVAL for a bad layer range, NULL or misaligned
+ * pointers, counts outside the limits above, slot ids outside the pool or repeated, strides below a request's tokens, buffers that overlap, more
+ * than 65535 requests or layers; CALVO_ENOMEM if a request needs more slots than the pool has or a buffer cannot be had. */
+int calvo_kv_evict(calvo_ctx* ctx, const calvo_evict_request* reqs, int n_reqs, int layer_begin, int layer_end, const float* mass, int32_t mass_rows,
+                   int64_t mass_stride, int32_t* kept, int64_t kept_stride, float* mass_out, int64_t out_stride);
+
 /* ---- Inter-request scheduling (paper Section 3.2; compared policies: Section 4.3).  Host code only.
  *
  * Cost model: a linear function of two variables fitted by offline profiling - loading latency linear in the

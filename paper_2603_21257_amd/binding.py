@@ -23,7 +23,8 @@ CALVO_EV_QUERY, CALVO_EV_HOST_WAIT, CALVO_EV_STREAM_WAIT = 0, 1, 2
 # CALVO_LIB names another build of the library (A/B timing of two builds); default: the in-tree one
 LIB_PATH = os.environ.get("CALVO_LIB") or os.path.join(os.path.dirname(os.path.abspath(__file__)), "libcalvo.so")
 EXPORTS = ["calvo_create", "calvo_destroy", "calvo_kv_ingest", "calvo_kv_ingest_chunked", "calvo_chunk_count",
-           "calvo_chunk_event", "calvo_kv_ingest_l3", "calvo_l3_wait", "calvo_layer_event", "calvo_prefill_attn", "calvo_prefill_attn_noalloc", "calvo_batch_prepare", "calvo_batch_destroy", "calvo_prefill_attn_batch", "calvo_attn_kernel_ms", "calvo_mfma_peak", "calvo_attn_kernel_info", "calvo_attn_tile_rows", "calvo_attn_plan", "calvo_attn_plan_items", "calvo_ingest_plan", "calvo_cost_fit", "calvo_cost_estimate",
+           "calvo_chunk_event", "calvo_kv_ingest_l3", "calvo_l3_wait", "calvo_layer_event", "calvo_prefill_attn", "calvo_prefill_attn_noalloc", "calvo_batch_prepare", "calvo_batch_destroy", "calvo_prefill_attn_batch",
+           "calvo_window_prepare", "calvo_window_destroy", "calvo_window_attn", "calvo_attn_mass", "calvo_kv_evict", "calvo_attn_kernel_ms", "calvo_mfma_peak", "calvo_attn_kernel_info", "calvo_attn_tile_rows", "calvo_attn_plan", "calvo_attn_plan_items", "calvo_ingest_plan", "calvo_cost_fit", "calvo_cost_estimate",
            "calvo_sched_pick", "calvo_sched_simulate", "calvo_pool_create", "calvo_pool_destroy", "calvo_pool_reserve",
            "calvo_pool_retain", "calvo_pool_release", "calvo_pool_counts", "calvo_pool_admit", "calvo_pool_retry",
            "calvo_pool_cancel", "calvo_dispatch_create", "calvo_dispatch_submit", "calvo_dispatch_wait", "calvo_dispatch_poll",
@@ -42,6 +43,16 @@ class calvo_config(C.Structure):
 class calvo_request(C.Structure):
     _fields_ = [("host_kv", C.c_void_p), ("host_layer_stride", C.c_int64), ("block_table", C.POINTER(C.c_int32)),
                 ("n_prefix_blocks", C.c_int32), ("first_ingest_block", C.c_int32), ("suffix_len", C.c_int32)]
+
+
+class calvo_window_request(C.Structure):
+    _fields_ = [("block_table", C.POINTER(C.c_int32)), ("n_cached", C.c_int32), ("n_new", C.c_int32), ("mass_row", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class calvo_evict_request(C.Structure):
+    _fields_ = [("src_table", C.POINTER(C.c_int32)), ("dst_table", C.POINTER(C.c_int32)), ("n_tokens", C.c_int32), ("n_keep", C.c_int32),
+                ("n_first", C.c_int32), ("n_last", C.c_int32), ("mass_row", C.c_int32), ("reserved", C.c_int32)]
 
 
 class calvo_l3_config(C.Structure):
@@ -123,6 +134,13 @@ def lib() -> C.CDLL:
         L.calvo_batch_destroy.argtypes = [C.c_void_p]
         L.calvo_prefill_attn_batch.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                                C.c_float]
+        L.calvo_window_prepare.argtypes = [C.c_void_p, C.POINTER(calvo_window_request), C.c_int, C.c_int32, C.c_int32, C.POINTER(C.c_void_p)]
+        L.calvo_window_destroy.argtypes = [C.c_void_p]
+        L.calvo_window_attn.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float]
+        L.calvo_attn_mass.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int32,
+                                      C.c_float]
+        L.calvo_kv_evict.argtypes = [C.c_void_p, C.POINTER(calvo_evict_request), C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int32, C.c_int64,
+                                     C.c_void_p, C.c_int64, C.c_void_p, C.c_int64]
         L.calvo_mfma_peak.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_double)]
         L.calvo_attn_kernel_ms.argtypes = [C.c_void_p, C.c_int, C.POINTER(C.c_float)]
         L.calvo_attn_plan.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int32,
@@ -306,6 +324,63 @@ def calvo_batch_destroy(batch: int) -> None:
 
 def calvo_prefill_attn_batch(ctx: int, batch: int, layer: int, q, k_suffix, v_suffix, out, scale: float = 0.0) -> None:
     _check(lib().calvo_prefill_attn_batch(ctx, batch, layer, _ptr(q), _ptr(k_suffix), _ptr(v_suffix), _ptr(out), float(scale)))
+
+
+# ---- a bounded cache: window attention, gathered weights, eviction
+
+def make_window_request(block_table, n_cached: int, n_new: int, mass_row: int = 0) -> calvo_window_request:
+    """Marshal one request of a window batch.  The returned struct keeps the table array alive."""
+    tab, tp = _i32(block_table)
+    if len(tab) < -(-(int(n_cached) + int(n_new)) // 16):
+        raise ValueError("block_table holds fewer slots than n_cached + n_new tokens need")
+    r = calvo_window_request(tp, int(n_cached), int(n_new), int(mass_row), 0)
+    r._keep = tab
+    return r
+
+
+def make_evict_request(src_table, n_tokens: int, dst_table, n_keep: int, n_first: int = 0, n_last: int = 0,
+                       mass_row: int = 0) -> calvo_evict_request:
+    """Marshal one request of an eviction.  The returned struct keeps the table arrays alive."""
+    src, sp = _i32(src_table)
+    dst, dp = _i32(dst_table)
+    if len(src) < -(-int(n_tokens) // 16) or len(dst) < -(-int(n_keep) // 16):
+        raise ValueError("a table holds fewer slots than its tokens need")
+    r = calvo_evict_request(sp, dp, int(n_tokens), int(n_keep), int(n_first), int(n_last), int(mass_row), 0)
+    r._keep = (src, dst)
+    return r
+
+
+def _struct_array(kind, reqs):
+    arr = (kind * max(len(reqs), 1))(*reqs)
+    arr._keep = list(reqs)
+    return arr
+
+
+def calvo_window_prepare(ctx: int, reqs: Sequence[calvo_window_request], window: int, n_first: int = 0) -> int:
+    """Checks, plans and uploads a batch for all layers of a step; returns the handle for calvo_window_attn and calvo_attn_mass."""
+    out = C.c_void_p()
+    _check(lib().calvo_window_prepare(ctx, _struct_array(calvo_window_request, reqs), len(reqs), int(window), int(n_first), C.byref(out)))
+    return out.value
+
+
+def calvo_window_destroy(window: int) -> None:
+    _check(lib().calvo_window_destroy(window))
+
+
+def calvo_window_attn(window: int, layer: int, q, k_new, v_new, out, lse=None, scale: float = 0.0) -> None:
+    _check(lib().calvo_window_attn(window, layer, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(lse), float(scale)))
+
+
+def calvo_attn_mass(window: int, layer: int, q, lse, mass_in, mass_out, mass_rows: int, mass_stride: int, last_rows: int = 0,
+                    scale: float = 0.0) -> None:
+    _check(lib().calvo_attn_mass(window, layer, _ptr(q), _ptr(lse), _ptr(mass_in), _ptr(mass_out), int(mass_rows), int(mass_stride),
+                                 int(last_rows), float(scale)))
+
+
+def calvo_kv_evict(ctx: int, reqs: Sequence[calvo_evict_request], layer_begin: int, layer_end: int, mass, mass_rows: int, mass_stride: int,
+                   kept, kept_stride: int, mass_out=None, out_stride: int = 0) -> None:
+    _check(lib().calvo_kv_evict(ctx, _struct_array(calvo_evict_request, reqs), len(reqs), layer_begin, layer_end, _ptr(mass), int(mass_rows),
+                                int(mass_stride), _ptr(kept), int(kept_stride), _ptr(mass_out), int(out_stride)))
 
 
 CALVO_MFMA_16x16x32, CALVO_MFMA_32x32x16 = 0, 1

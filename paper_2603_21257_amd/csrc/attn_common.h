@@ -23,6 +23,11 @@ __device__ inline WorkItem load_item(const WorkItem* items, int i) {
   return {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
 }
 
+__device__ inline WinItem load_win_item(const WinItem* items, int i) {
+  const const_i32p w = (const_i32p)(uintptr_t)(items + i);
+  return {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7], w[8], w[9], w[10], {0, 0, 0, 0, 0}};
+}
+
 constexpr int kD = 128;
 constexpr int kSK = 32;                        // keys per sub-tile / ring slot
 constexpr int kRow = 256;                      // bytes per token row of one head

@@ -122,6 +122,7 @@ void destroy_partial(calvo_ctx* c) {
   if (c->part_o) (void)hipFree(c->part_o);
   if (c->part_ml) (void)hipFree(c->part_ml);
   for (auto& b : c->blob_free) { (void)hipFree(b.d); (void)hipHostFree(b.h); }
+  for (auto& b : c->step_free) { (void)hipFree(b.d); (void)hipHostFree(b.h); (void)hipEventDestroy(b.read); }
   for (auto& s : c->s_copy) if (s) (void)hipStreamDestroy(s);
   if (c->s_scatter) (void)hipStreamDestroy(c->s_scatter);
   if (c->own_compute && c->s_compute) (void)hipStreamDestroy(c->s_compute);
@@ -320,6 +321,36 @@ bool layer_is_issued(calvo_ctx* c, int layer) {
 
 namespace calvo {
 namespace host {
+
+int queue_behind_layer(calvo_ctx* c, int layer) {
+  const int rc = wait_handed_over(c, layer);
+  if (rc != CALVO_OK) return rc;
+  if (!layer_is_issued(c, layer)) return CALVO_OK;
+  hipStreamCaptureStatus s = hipStreamCaptureStatusNone;
+  HIP_TRY(hipStreamIsCapturing(c->s_compute, &s));
+  if (s == hipStreamCaptureStatusNone) {
+    HIP_TRY(hipStreamWaitEvent(c->s_compute, c->ev_layer[layer], 0));
+    return CALVO_OK;
+  }
+  hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;         // the question touches no captured work
+  HIP_TRY(hipThreadExchangeStreamCaptureMode(&mode));
+  const hipError_t e = hipEventQuery(c->ev_layer[layer]);
+  (void)hipThreadExchangeStreamCaptureMode(&mode);
+  if (e == hipSuccess) return CALVO_OK;
+  (void)hipGetLastError();
+  if (e != hipErrorNotReady) return fail_hip(e, "hipEventQuery(layer)");
+  return fail(CALVO_ENOTREADY, "layer %d is still being loaded, which a captured call cannot wait for", layer);
+}
+
+int window_kernels_ready(calvo_ctx* c) {
+  if (c->window_kernels) return CALVO_OK;
+  const bool f32 = c->cfg.dtype == CALVO_F32;
+  HIP_TRY(attn_window_prepare(c->cfg.dtype, c->cfg.head_dim, attn_rows_shape(f32, c->cfg.head_dim, false).tile_rows));
+  if (attn_rows_has_large(f32, c->cfg.head_dim))
+    HIP_TRY(attn_window_prepare(c->cfg.dtype, c->cfg.head_dim, attn_rows_shape(f32, c->cfg.head_dim, true).tile_rows));
+  c->window_kernels = true;
+  return CALVO_OK;
+}
 
 // L2->L1 for nb consecutive blocks (nb <= staging_blocks) that sit in page-locked host memory:
 // copy engine into the next device staging buffer, then scatter into the pool through the table.

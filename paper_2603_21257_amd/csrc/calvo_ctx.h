@@ -13,6 +13,18 @@
 #include "../../include/calvo.h"
 #include "calvo_internal.h"
 
+namespace calvo {
+// Descriptors and partial results of one batch or call (calvo_window.hip): device memory, its pinned source, and the event behind the
+// upload, after which the source may be written again
+struct StepBuf {
+  int32_t* d = nullptr;
+  int32_t* h = nullptr;
+  size_t d_bytes = 0, h_bytes = 0;
+  hipEvent_t read = nullptr;
+  bool pending = false;
+};
+}  // namespace calvo
+
 struct calvo_ctx {
   calvo_config cfg{};
   size_t elt = 0, blk_bytes = 0;
@@ -105,6 +117,11 @@ struct calvo_ctx {
   struct BlobBuf { int32_t* d; int32_t* h; size_t bytes; };
   std::mutex blob_mu;
   std::vector<BlobBuf> blob_free;
+  std::vector<calvo::StepBuf> step_free;      // of calvo_window.hip, given back (guarded by blob_mu)
+  // per slot: the mark of the last table check that met it (calvo_window.hip); a check takes marks that no slot carries
+  std::vector<uint32_t> slot_marks;
+  uint32_t next_mark = 1;
+  bool window_kernels = false;               // their LDS limits are raised
   std::vector<void*> l2_ring;
   std::vector<hipEvent_t> ev_l2_free;
   std::vector<char> l2_free_recorded;
@@ -142,6 +159,13 @@ int upload_ingest_table(calvo_ctx* c, const int32_t* slots, size_t n);
 int ensure_l2_ring(calvo_ctx* c, size_t slot_bytes, int n_slots);
 
 void parallel_copy(unsigned char* dst, const unsigned char* src, size_t n, int n_threads);
+
+// Queues the compute stream behind the layer's most recent load (with a running L3 loader after a wait for its hand-over).  While the
+// stream is captured nothing outside can be waited for: CALVO_ENOTREADY unless the layer is in.
+int queue_behind_layer(calvo_ctx* c, int layer);
+
+// Raises the LDS limits of the window kernels for the context's shape, once
+int window_kernels_ready(calvo_ctx* c);
 
 // The compute stage of one layer.  use_static: descriptors and partial results in the static device
 // array (calvo_prefill_attn_noalloc).  ready: NULL = wait for the layer's own loading state (events of

@@ -118,6 +118,84 @@ struct RowsParams {
 hipError_t attn_rows_prepare(int dtype, int head_dim, int tile_rows);
 hipError_t launch_attn_rows(const RowsParams& p, int dtype, int tile_rows, int n_items, const int32_t* split_tiles, int n_split_tiles,
                             hipStream_t stream);
+// ---- attention with a window and first tokens (attn_window.hip), gathered weights (attn_mass.hip), eviction (kv_evict.hip)
+
+// A work item of the attention: one tile of new tokens of one request over part of the keys that it sees.  The tile's keys are first_subs
+// sub-tiles of 32 that hold first tokens, from position 0 on, and the sub-tiles from 32 * (first_subs + gap) on; [sub_begin, sub_end) counts
+// through both.  What the kernels need of the request is here: no descriptor load in front of the block table.
+struct WinItem {
+  int32_t q_tile, sub_begin, sub_end;
+  int32_t n_splits, first_item;        // pieces the tile is cut into, index of the first
+  int32_t table_off, n_cached, n_new, q_off;
+  int32_t first_subs, gap;
+  int32_t pad[5];
+};
+static_assert(sizeof(WinItem) == 64, "one cache line half");
+
+struct WinParams {
+  const void* q;
+  void* out;
+  float* lse;                // or NULL: log-sum-exp of every row, [tokens][query heads]
+  void* pool_layer;
+  const WinItem* items;
+  const int32_t* tables;
+  int32_t n_q_heads, n_kv_heads, head_dim;
+  uint32_t group;            // query heads per KV head
+  int32_t window, n_first;
+  float scale;
+  float* part_o;             // partial results of cut tiles as in RowsParams
+  float* part_ml;
+};
+// raises the kernels' dynamic LDS limit; before the first launch on a device
+hipError_t attn_window_prepare(int dtype, int head_dim, int tile_rows);
+hipError_t launch_attn_window(const WinParams& p, int dtype, int tile_rows, int n_items, const int32_t* split_tiles, int n_split_tiles,
+                              hipStream_t stream);
+
+// One request of a window batch, device memory
+struct WinReq {
+  int32_t table_off, n_cached, n_new, q_off, mass_row;
+  int32_t first_tile;        // of the request's key tiles among those of the batch (attn_mass.hip)
+  int32_t pad[2];
+};
+struct MassParams {
+  const void* q;
+  const float* lse;
+  const float* mass_in;      // or NULL: zeros
+  float* mass_out;
+  const void* pool_layer;
+  const WinReq* reqs;
+  const int32_t* tables;
+  int64_t mass_stride;       // floats from one KV head's row to the next
+  int32_t n_reqs, n_tiles;
+  int32_t n_q_heads, n_kv_heads, head_dim;
+  uint32_t group;
+  int32_t window, n_first, last_rows;   // last_rows: 0 = all
+  float scale;
+};
+int attn_mass_tile_keys(int dtype, int head_dim);
+hipError_t launch_attn_mass(const MassParams& p, int dtype, hipStream_t stream);
+
+// One request of an eviction, device memory
+struct EvictDesc {
+  int32_t src_off, dst_off;  // of its tables inside the table array
+  int32_t n_tokens, n_keep, n_first, n_last, mass_row;
+  int32_t pad;
+};
+struct EvictParams {
+  unsigned char* pool;       // first layer of the call
+  const EvictDesc* reqs;
+  const int32_t* tables;
+  const float* mass;         // [layers][mass rows][KV heads][mass_stride]
+  float* mass_out;           // or NULL; the same with out_stride
+  int32_t* kept;             // [layers][requests][KV heads][kept_stride]
+  int64_t layer_bytes, mass_layer, mass_stride, out_layer, out_stride, kept_stride;
+  int32_t n_reqs, n_layers, n_kv_heads;
+  int32_t row_chunks;        // 16-byte chunks of one head's K (or V) of a token
+  int32_t max_keep;          // most tokens that a request keeps
+};
+hipError_t launch_evict_select(const EvictParams& p, hipStream_t stream);
+hipError_t launch_evict_move(const EvictParams& p, hipStream_t stream);
+
 // The pipelined bf16 / head-dim-128 kernels (attn_pipeline.h).  The *_prepare calls raise the
 // kernels' dynamic LDS limit; once per device, before the first launch.
 hipError_t attn_pipe_prepare();
