@@ -25,7 +25,7 @@ __device__ inline WorkItem load_item(const WorkItem* items, int i) {
 
 __device__ inline WinItem load_win_item(const WinItem* items, int i) {
   const const_i32p w = (const_i32p)(uintptr_t)(items + i);
-  return {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7], w[8], w[9], w[10], {0, 0, 0, 0, 0}};
+  return {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7], w[8], w[9], w[10], w[11], w[12], w[13], w[14], w[15]};
 }
 
 constexpr int kD = 128;
@@ -71,6 +71,9 @@ __device__ inline float quad_sum(float v) {
   v += __shfl_xor(v, 16, 64);
   return half_swap_sum(v);
 }
+
+// natural logarithm of a sum of exponentials: the sum l of 2^(x - m)
+__device__ inline float log_sum(float m, float l) { return (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f; }
 
 // two weights rounded to bf16 (nearest even), packed
 __device__ inline unsigned pack_bf16(float a, float b) {

@@ -104,7 +104,21 @@ struct PipeCfg {
   static constexpr int UNROLL = RING_ % 2 ? 2 * RING_ : RING_;
   static constexpr int PD = 4;         // LDS operand reads run this many operands ahead
   static constexpr int LDS_BYTES = 2 * RING_ * kSlot;
+  static constexpr bool WIN = false;
+  typedef AttnParams Params;
 };
+
+// With a window and first tokens (attn_window_pipe.hip).  Steady are the sub-tiles that every row of the tile sees in full; those that
+// first tokens end in, that the rows' windows begin in and that lie on the diagonal come behind them (WinItem).  The order of the keys does not
+// matter to a softmax.
+template <int NW_, int RING_, int HB_>
+struct WinPipeCfg : PipeCfg<NW_, RING_, HB_> {
+  static constexpr bool WIN = true;
+  typedef WinParams Params;
+};
+// WIN: the reference of a row that has seen no key.  Finite, so that the weight of a hidden key (score -inf) is 0 against it; far enough below
+// every score for the first visible one to pass the bound.
+constexpr float kNoRef = -3e38f;
 
 // m0 = lds_base + off for the dma_1k_m0 that follows at least one instruction later
 template <int OFF>
@@ -179,7 +193,9 @@ __device__ inline float max_of(const float (&v)[2]) {
 }
 
 template <class Cfg_>
-__device__ __forceinline__ void attn_pipeline(const AttnParams& p, unsigned char* smem) {
+__device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, unsigned char* smem) {
+  constexpr bool WIN = Cfg_::WIN;
+  constexpr float kUnset = WIN ? kNoRef : -INFINITY;
   constexpr int NW = Cfg_::NW, HB = Cfg_::HB, QB = Cfg_::QB, RING = Cfg_::RING, KA = Cfg_::KA, VA = Cfg_::VA, NI = Cfg_::NI, PD = Cfg_::PD;
   constexpr bool ACC = HB == 2;
   constexpr int kVBase = RING * kSlot;                 // V ring follows the K ring
@@ -207,9 +223,19 @@ __device__ __forceinline__ void attn_pipeline(const AttnParams& p, unsigned char
       it = bid / NHG;
     }
   }
-  if (p.item_index) it = p.item_index[it];
-  const WorkItem wi = p.items[it];
-  const ReqDesc rd = p.reqs[wi.req];
+  WorkItem wi;
+  ReqDesc rd;
+  int first_subs = 0, gap = 0, n_full = 0;             // WIN
+  if constexpr (WIN) {
+    const WinItem ww = load_win_item(p.items, it);
+    first_subs = ww.first_subs; gap = ww.gap; n_full = ww.n_full;
+    wi = {0, ww.q_tile, ww.sub_begin, ww.sub_end, ww.n_splits, ww.first_item, ww.q_off, ww.n_new};
+    rd = {ww.table_off, ww.n_cached, ww.n_new, ww.q_off};
+  } else {
+    if (p.item_index) it = p.item_index[it];
+    wi = p.items[it];
+    rd = p.reqs[wi.req];
+  }
   const int P = rd.prefix_len, S = rd.suffix_len;
   const int TQ = 32 * TPW;
   const int q_base = wi.q_tile * TQ;
@@ -228,7 +254,7 @@ __device__ __forceinline__ void attn_pipeline(const AttnParams& p, unsigned char
   const int ctx_len = P + S;
   const int jb = wi.sub_begin;
   const int n_sub = wi.sub_end - jb;
-  const int n_pipe = max(0, min(wi.sub_end, (P + q_base + 1) / kSK) - jb);
+  const int n_pipe = max(0, min(wi.sub_end, WIN ? n_full : (P + q_base + 1) / kSK) - jb);
   const int last_blk = (ctx_len + kBlockTokens - 1) / kBlockTokens - 1;
   typedef const __attribute__((address_space(4))) int64_t* const_i64p;
   const int n_blk_pad = last_blk + 1 + kTablePad + ((last_blk + 1) & 1);
@@ -250,13 +276,16 @@ __device__ __forceinline__ void attn_pipeline(const AttnParams& p, unsigned char
   }
   const unsigned dma_lds = lds0 + wave * (1024 * NI);
 
-  auto fetch_off = [&](int j) -> int64_t { return boffs[jb + j]; };
+  auto fetch_off = [&](int j) -> int64_t {
+    if constexpr (WIN) return boffs[jb + j < first_subs ? jb + j : jb + j + gap];
+    else return boffs[jb + j];
+  };
   // Where the launch takes the suffix along, its rows are read from the caller's arrays: a 16-key block lies wholly in the
   // prefix or wholly in the suffix.  The first tile of a suffix meets such blocks on its diagonal only, later ones (SFX) in
   // the pipelined part as well.  There the turns within the prefix come first, those that choose an address after them: 4096+700
   // tokens 55.0 us a call, with the choice in every turn 58.5; 448+400 13.8, with run-time ring slots outside the prefix 15.6.
   constexpr bool SFX = Cfg_::SFX;
-  typedef const __attribute__((address_space(4))) AttnParams* const_paramsp;
+  typedef const __attribute__((address_space(4))) typename Cfg_::Params* const_paramsp;
   const int p_blk = P / kBlockTokens;
   const int n_pool = SFX ? max(0, min(n_pipe, p_blk / 2 - jb)) : n_pipe;     // pipelined sub-tiles that lie in the prefix
   // Addresses of the request's suffix block 0 in the caller's arrays, as bases for voff_k and voff_v
@@ -310,7 +339,7 @@ __device__ __forceinline__ void attn_pipeline(const AttnParams& p, unsigned char
   f32x4 o[8][QB];
   float m_run[QB], l_run[QB];
 #pragma unroll
-  for (int qb = 0; qb < QB; qb++) { m_run[qb] = -INFINITY; l_run[qb] = 0.f; }
+  for (int qb = 0; qb < QB; qb++) { m_run[qb] = kUnset; l_run[qb] = 0.f; }
 
   // ---- lane-constant operand addresses inside a slot
   const lds_u8* ka_addr[4];
@@ -357,7 +386,7 @@ __device__ __forceinline__ void attn_pipeline(const AttnParams& p, unsigned char
         const int qb = QB0 + q;
         const float m_new = fmaxf(m_run[qb], __builtin_fmaf(row_max(s[0][q], s[1][q]), c2, kRefShift));
         alpha[q] = __builtin_amdgcn_exp2f(m_run[qb] - m_new);
-        changed |= m_run[qb] != -INFINITY && !(alpha[q] == 1.f);         // without a reference O is 0
+        changed |= m_run[qb] != kUnset && !(alpha[q] == 1.f);         // without a reference O is 0
         m_run[qb] = m_new;
         l_run[qb] = l_run[qb] * alpha[q];
         weights_of(s[0][q], s[1][q], qb, ps[q], pw[q]);
@@ -512,7 +541,8 @@ __device__ __forceinline__ void attn_pipeline(const AttnParams& p, unsigned char
   };
 
   // ---- fill: one sub-tile of K or of V into its slot
-  const SuffixBases sfx0 = suffix_bases(p.k_suffix, p.v_suffix);
+  SuffixBases sfx0{};
+  if constexpr (!WIN) sfx0 = suffix_bases(p.k_suffix, p.v_suffix);
   auto request_k = [&](auto j) {
     constexpr int J = decltype(j)::value;
     const int sub = min(J, n_pipe - 1);
@@ -580,7 +610,8 @@ __device__ __forceinline__ void attn_pipeline(const AttnParams& p, unsigned char
         static_for<0, PD>([&](auto idx) { pre[decltype(idx)::value] = load_opnd(idx, Tag<2>{}, Tag<0>{}); });
         constexpr int U = Cfg_::UNROLL;
         const_paramsp ps = (const_paramsp)__builtin_amdgcn_kernarg_segment_ptr();
-        const SuffixBases sfx = suffix_bases(ps->k_suffix, ps->v_suffix);
+        SuffixBases sfx{};
+        if constexpr (!WIN) sfx = suffix_bases(ps->k_suffix, ps->v_suffix);
         if (t + U < n_pipe) {
           // offsets of sub-tiles t + VA .. t + KA + RING - 1
           int64_t off_cur[U + DV], off_nxt[U];
@@ -624,11 +655,25 @@ __device__ __forceinline__ void attn_pipeline(const AttnParams& p, unsigned char
   asm volatile("" : "+s"(pe));
 
   // ---- sub-tiles on or past the diagonal: requested in groups of at most RING - 2
-  const unsigned char* ks = (const unsigned char*)pe->k_suffix;
-  const unsigned char* vs = (const unsigned char*)pe->v_suffix;
+  const unsigned char *ks = nullptr, *vs = nullptr;
+  if constexpr (!WIN) {
+    ks = (const unsigned char*)pe->k_suffix;
+    vs = (const unsigned char*)pe->v_suffix;
+  }
+  // where sub-tile j of the tail lies in the context; the item is read again: what describes its tail is not kept through the loop
+  WinItem ww{};
+  if constexpr (WIN) ww = load_win_item(pe->items, it);
+  auto tail_sub = [&](int j) -> int {
+    if constexpr (WIN) {
+      const int x = jb + j - ww.n_full;
+      return x < ww.n_part ? pe->n_first / kSK : x < ww.n_part + ww.n_edge ? ww.edge + x - ww.n_part : ww.diag + x - ww.n_part - ww.n_edge;
+    }
+    return jb + j;
+  };
   auto request_tail = [&](int j) {
-    const int sfx_blk = 2 * (jb + j) + wblk - P / kBlockTokens;
-    const int64_t boff = fetch_off(j);
+    const int sub = tail_sub(j);
+    const int sfx_blk = 2 * sub + wblk - P / kBlockTokens;
+    const int64_t boff = boffs[sub];
     const unsigned char *kb = pool + boff, *vb = kb;
     if (ks && sfx_blk >= 0) {
       const int64_t soff = (int64_t)rd.q_off * row_b + (int64_t)sfx_blk * half_b;
@@ -637,7 +682,7 @@ __device__ __forceinline__ void attn_pipeline(const AttnParams& p, unsigned char
     }
 #pragma unroll
     for (int h = 0; h < NI; h++) {
-      const bool live = (jb + j) * kSK + wblk * 16 + brow0 + 4 * h < ctx_len;
+      const bool live = sub * kSK + wblk * 16 + brow0 + 4 * h < ctx_len;
       const unsigned l_k = __builtin_amdgcn_readfirstlane(dma_lds + ring_slot(j) * kSlot + h * 1024);
       if (live) {
         dma_1k(scalar_ptr(kb), voff_k[h], l_k);
@@ -667,6 +712,20 @@ __device__ __forceinline__ void attn_pipeline(const AttnParams& p, unsigned char
       pv_all(ring_slot(t + 1), pb[0]);
     }
   }
+  // WIN: V of the sub-tile in tail slot j holds an infinity or a NaN (a lane looks at half a row).  The product takes weight 0 times such a
+  // V for a NaN, also in rows that do not see the key.
+  auto v_not_finite = [&](int j) -> bool {
+    const lds_u8* half_row = lds + kVBase + ring_slot(j) * kSlot + lane * 128;
+    unsigned bad = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const u32x4 x = *(const __attribute__((address_space(3))) u32x4*)(half_row + ((i + (lane >> 1)) & 7) * 16);
+#pragma unroll
+      for (int e = 0; e < 4; e++) bad |= (x[e] & 0x7f807f80u) + 0x00800080u;      // an exponent of ones carries into the sign
+    }
+    return __builtin_amdgcn_ballot_w64((bad & 0x80008000u) != 0) != 0;
+  };
+  bool walk = false;
   for (int j0 = n_pipe; j0 < n_sub; j0 += TG) {
     if (j0 > n_pipe) {
       __syncthreads();                                   // everyone has read the group before
@@ -675,15 +734,30 @@ __device__ __forceinline__ void attn_pipeline(const AttnParams& p, unsigned char
     wait_vm<0>();
     __syncthreads();
     for (int j = j0; j < min(n_sub, j0 + TG); j++) {
-      const int k0 = (jb + j) * kSK;
+      const int k0 = tail_sub(j) * kSK;
+      if constexpr (WIN) walk |= v_not_finite(j);
       // row block by row block: V of a sub-tile that a block sees nothing of stays away from it (0 times infinity)
       static_for<0, HB>([&](auto hh) {
         constexpr int H = decltype(hh)::value;
         const int pq_min = P + wq0[H];
         if (!(wq0[H] < S && k0 <= P + min(wq0[H] + 32, S) - 1)) return;
+        if constexpr (WIN) {
+          if (k0 + 31 <= pq_min - pe->window && k0 >= pe->n_first) return;
+        }
         f32x4 s2[2][2];
         qk(ring_slot(j), Tag<2 * H>{}, s2);
-        if (k0 + 31 > pq_min) {
+        if constexpr (WIN) {
+          const int window = pe->window, n_first = pe->n_first;
+#pragma unroll
+          for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+            for (int q = 0; q < 2; q++)
+#pragma unroll
+              for (int r = 0; r < 4; r++) {
+                const int key = k0 + 16 * kb + 4 * g + r, pos = pq_min + 16 * q + c;
+                if (key > pos || (key <= pos - window && key >= n_first)) s2[kb][q][r] = -INFINITY;
+              }
+        } else if (k0 + 31 > pq_min) {
 #pragma unroll
           for (int kb = 0; kb < 2; kb++)
 #pragma unroll
@@ -695,6 +769,85 @@ __device__ __forceinline__ void attn_pipeline(const AttnParams& p, unsigned char
         bf16x8 pw[2];
         softmax(Tag<2 * H>{}, s2, pw);
         pv(ring_slot(j), Tag<2 * H>{}, Tag<2>{}, pw);
+      });
+    }
+  }
+
+  // ---- WIN: a tail that holds such V.  The wave's rows meet the piece's keys again, 16 rows and 16 keys at a time and V key by key: a row adds
+  // weight times V of the keys that it sees and touches no other.  Rare, so it is written for few registers.
+  if constexpr (WIN) {
+    if (__builtin_expect(walk, 0)) {
+      const const_i64p offs = (const_i64p)(uintptr_t)(pe->blk_offs + rd.table_off);
+      const unsigned char* pool_w = (const unsigned char*)pe->pool_layer;
+      const int window = pe->window, n_first = pe->n_first;
+      static_for<0, QB>([&](auto qtag) {
+        constexpr int qb = decltype(qtag)::value;
+        const int pos = P + wq0[qb >> 1] + 16 * (qb & 1) + c;
+        auto hidden = [&](int key) { return key > pos || (key <= pos - window && key >= n_first); };
+        f32x4 acc[8];
+#pragma unroll
+        for (int db = 0; db < 8; db++) acc[db] = zero4;
+        float m = kNoRef, l = 0.f;
+#pragma unroll 1
+        for (int jj = 0; jj < 2 * n_sub; jj++) {
+          const int j = jj >> 1, v = jb + j;
+          const int sub = j < n_pipe ? (v < ww.first_subs ? v : v + ww.gap) : tail_sub(j);
+          const int b = 2 * sub + (jj & 1), key0 = kBlockTokens * b;
+          const int rest = min(kBlockTokens, ctx_len - key0);
+          if (rest <= 0) continue;
+          const unsigned char* kp = pool_w + offs[(b & 1) * (n_blk_pad >> 1) + (b >> 1)] + kv * kRow;
+          const unsigned char* kr = kp + (int64_t)min(c, rest - 1) * row_b + 16 * g;
+          bf16x8 kx[4];
+#pragma unroll
+          for (int ks = 0; ks < 4; ks++) {
+            kx[ks] = *(const bf16x8*)(kr + 64 * ks);
+            pin(kx[ks]);
+          }
+          mfma_settle();
+          f32x4 s;
+#pragma unroll
+          for (int ks = 0; ks < 4; ks++) {
+            pin(kx[ks]);
+            if (ks == 0) mfma_first(s, kx[ks], qB[qb][ks]);
+            else mfma_next(s, kx[ks], qB[qb][ks]);
+          }
+          mfma_settle();
+          pin(s);
+          float w[4], mx = -INFINITY;
+#pragma unroll
+          for (int r = 0; r < 4; r++) {
+            if (hidden(key0 + 4 * g + r)) s[r] = -INFINITY;
+            mx = fmaxf(mx, s[r]);
+          }
+          const float mn = fmaxf(m, quad_max(mx) * c2), alpha = __builtin_amdgcn_exp2f(m - mn);
+          l *= alpha;
+          m = mn;
+#pragma unroll
+          for (int db = 0; db < 8; db++) acc[db] *= alpha;
+#pragma unroll
+          for (int r = 0; r < 4; r++) {
+            w[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, -m));
+            l += w[r];
+          }
+#pragma unroll 1
+          for (int t = 0; t < rest; t++) {
+            const float mine = t & 2 ? (t & 1 ? w[3] : w[2]) : (t & 1 ? w[1] : w[0]);
+            const float wk = __shfl(mine, 16 * (t >> 2) + c);
+            if (hidden(key0 + t)) continue;
+            const unsigned char* vr = kp + half_b + (int64_t)t * row_b + 8 * g;
+#pragma unroll
+            for (int db = 0; db < 8; db++) {
+              const u32x2 x = *(const u32x2*)(vr + 32 * db);
+#pragma unroll
+              for (int r = 0; r < 4; r++)
+                acc[db][r] = __builtin_fmaf(wk, __builtin_bit_cast(float, r & 1 ? x[r >> 1] & 0xffff0000u : x[r >> 1] << 16), acc[db][r]);
+            }
+          }
+        }
+        m_run[qb] = m;
+        l_run[qb] = l;
+#pragma unroll
+        for (int db = 0; db < 8; db++) o[db][qb] = acc[db];
       });
     }
   }
@@ -712,16 +865,21 @@ __device__ __forceinline__ void attn_pipeline(const AttnParams& p, unsigned char
       if (tokq < S) {
         const int64_t prow = slot * 32 + 16 * (qb & 1) + c;
         store_piece(pe->part_o + prow * kD, g, o, qb);
-        if (g == 0) *(f32x2*)(pe->part_ml + prow * 2) = (f32x2){m_run[qb], P + tokq < jb * kSK ? 0.f : lt};
+        if (g == 0) *(f32x2*)(pe->part_ml + prow * 2) = (f32x2){m_run[qb], !WIN && P + tokq < jb * kSK ? 0.f : lt};
       }
     } else {
       const float inv = 1.f / lt;
+      if constexpr (WIN) {
+        if (pe->lse && g == 0 && tokq < S) pe->lse[(int64_t)(rd.q_off + tokq) * Hq + hq[qb >> 1]] = log_sum(m_run[qb], lt);
+      }
       unsigned short* row = (unsigned short*)pe->out + ((int64_t)(rd.q_off + tokq) * Hq + hq[qb >> 1]) * kD;
 #pragma unroll
       for (int d = 0; d < 4; d++) store_out(row, d, g, o[2 * d][qb], o[2 * d + 1][qb], inv, tokq < S);
     }
   }
-  if (threadIdx.x == 0) clock_end(pe->clock.words);
+  if constexpr (!WIN) {
+    if (threadIdx.x == 0) clock_end(pe->clock.words);
+  }
 }
 
 }  // namespace attn

@@ -95,8 +95,6 @@ __device__ inline float as_float(unsigned x) { return __builtin_bit_cast(float, 
 __device__ inline unsigned bf16_rne(float x) {
   return (unsigned)__builtin_bit_cast(unsigned short, (__bf16)x);
 }
-// natural logarithm of a sum of exponentials: the sum l of 2^(x - m)
-__device__ inline float log_sum(float m, float l) { return (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f; }
 __device__ inline float bf16_widen(unsigned b) { return __builtin_bit_cast(float, b << 16); }
 
 template <class C>

@@ -348,6 +348,7 @@ int window_kernels_ready(calvo_ctx* c) {
   HIP_TRY(attn_window_prepare(c->cfg.dtype, c->cfg.head_dim, attn_rows_shape(f32, c->cfg.head_dim, false).tile_rows));
   if (attn_rows_has_large(f32, c->cfg.head_dim))
     HIP_TRY(attn_window_prepare(c->cfg.dtype, c->cfg.head_dim, attn_rows_shape(f32, c->cfg.head_dim, true).tile_rows));
+  if (!f32 && c->cfg.head_dim == 128) HIP_TRY(attn_window_pipe_prepare());
   c->window_kernels = true;
   return CALVO_OK;
 }

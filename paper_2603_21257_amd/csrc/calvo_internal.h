@@ -120,17 +120,20 @@ hipError_t launch_attn_rows(const RowsParams& p, int dtype, int tile_rows, int n
                             hipStream_t stream);
 // ---- attention with a window and first tokens (attn_window.hip), gathered weights (attn_mass.hip), eviction (kv_evict.hip)
 
-// A work item of the attention: one tile of new tokens of one request over part of the keys that it sees.  The tile's keys are first_subs
-// sub-tiles of 32 that hold first tokens, from position 0 on, and the sub-tiles from 32 * (first_subs + gap) on; [sub_begin, sub_end) counts
-// through both.  What the kernels need of the request is here: no descriptor load in front of the block table.
+// A work item of the attention: one tile of new tokens of one request over part of the keys that it sees, [sub_begin, sub_end) of a list of
+// 32-key sub-tiles.  What the kernels need of the request is here: no descriptor load in front of the block table.
+// Packed rows: the list is first_subs sub-tiles that hold first tokens, from position 0 on, and those from first_subs + gap on.
+// Pipelined kernels: it begins with the n_full sub-tiles that every row of the tile sees in full - first_subs of first tokens, then those
+// from first_subs + gap on - and ends with the others: n_part (0 or 1) that first tokens end in, n_edge from edge on that the rows'
+// windows begin in, and those from diag on.
 struct WinItem {
   int32_t q_tile, sub_begin, sub_end;
   int32_t n_splits, first_item;        // pieces the tile is cut into, index of the first
   int32_t table_off, n_cached, n_new, q_off;
   int32_t first_subs, gap;
-  int32_t pad[5];
+  int32_t n_full, n_part, edge, n_edge, diag;
 };
-static_assert(sizeof(WinItem) == 64, "one cache line half");
+static_assert(sizeof(WinItem) == 64, "16 words, as load_win_item reads them");
 
 struct WinParams {
   const void* q;
@@ -138,9 +141,11 @@ struct WinParams {
   float* lse;                // or NULL: log-sum-exp of every row, [tokens][query heads]
   void* pool_layer;
   const WinItem* items;
-  const int32_t* tables;
+  const int32_t* tables;     // packed rows: what table_off of an item counts in ...
+  const int64_t* blk_offs;   // ... pipelined: this, as AttnParams has it
   int32_t n_q_heads, n_kv_heads, head_dim;
   uint32_t group;            // query heads per KV head
+  int32_t heads_per_wg, row_blocks_per_wg;   // pipelined: as AttnParams
   int32_t window, n_first;
   float scale;
   float* part_o;             // partial results of cut tiles as in RowsParams
@@ -150,11 +155,20 @@ struct WinParams {
 hipError_t attn_window_prepare(int dtype, int head_dim, int tile_rows);
 hipError_t launch_attn_window(const WinParams& p, int dtype, int tile_rows, int n_items, const int32_t* split_tiles, int n_split_tiles,
                               hipStream_t stream);
+// the same on the pipelined bodies, bf16 and 128-wide heads; variant: kAttnPipe or kAttnDuo (attn_window_pipe.hip)
+hipError_t attn_window_pipe_prepare();
+hipError_t launch_attn_window_pipe(const WinParams& p, int variant, int n_items, const int32_t* split_tiles, int n_split_tiles, hipStream_t stream);
 
-// One request of a window batch, device memory
-struct WinReq {
+// A work item of the gathered weights: key tile `tile` of a request (attn_mass_tile_keys keys) and those of the new tokens [begin, end) whose rows
+// see it.  part: where the sums go if the tile has several items, else -1
+struct MassItem {
   int32_t table_off, n_cached, n_new, q_off, mass_row;
-  int32_t first_tile;        // of the request's key tiles among those of the batch (attn_mass.hip)
+  int32_t tile, begin, end, part;
+  int32_t pad[3];
+};
+// A key tile with several items: its sums are n_parts from part on
+struct MassAdd {
+  int32_t n_cached, n_tokens, mass_row, tile, part, n_parts;
   int32_t pad[2];
 };
 struct MassParams {
@@ -163,17 +177,18 @@ struct MassParams {
   const float* mass_in;      // or NULL: zeros
   float* mass_out;
   const void* pool_layer;
-  const WinReq* reqs;
+  const MassItem* items;
   const int32_t* tables;
+  float* part;               // [part][KV head][keys of a tile]
   int64_t mass_stride;       // floats from one KV head's row to the next
-  int32_t n_reqs, n_tiles;
+  int32_t n_items;
   int32_t n_q_heads, n_kv_heads, head_dim;
   uint32_t group;
   int32_t window, n_first, last_rows;   // last_rows: 0 = all
   float scale;
 };
 int attn_mass_tile_keys(int dtype, int head_dim);
-hipError_t launch_attn_mass(const MassParams& p, int dtype, hipStream_t stream);
+hipError_t launch_attn_mass(const MassParams& p, int dtype, const MassAdd* adds, int n_adds, hipStream_t stream);
 
 // One request of an eviction, device memory
 struct EvictDesc {

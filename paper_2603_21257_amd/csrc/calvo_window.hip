@@ -2,6 +2,7 @@
 // weights, eviction (include/calvo.h).  Validation, the plan of a batch and its description to the device, the launches.
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 #include <cstring>
 #include <new>
 
@@ -19,12 +20,12 @@ struct calvo_window {
   int64_t longest = 0;                  // most tokens of a request, new ones included
   int max_mass_row = -1;
   bool mass_rows_differ = true;
-  int key_tiles = 0;                    // of attn_mass.hip
   WindowPlan plan;
+  MassPlan mass;
   StepBuf buf;
   // 32-bit words from the beginning of buf.d
-  size_t items_at = 0, split_at = 0, reqs_at = 0, append_at = 0, tables_at = 0;
-  size_t part_o_at = 0, part_ml_at = 0; // floats, behind them
+  size_t items_at = 0, split_at = 0, mass_at = 0, add_at = 0, append_at = 0, tables_at = 0, offs_at = 0;
+  size_t part_o_at = 0, part_ml_at = 0, part_mass_at = 0; // floats, behind them
 };
 
 namespace {
@@ -209,65 +210,90 @@ int window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, i
   std::vector<WindowLens> lens((size_t)n_reqs);
   std::vector<int32_t> rows_used;
   int64_t table_words = 0;
-  const int tile_keys = attn_mass_tile_keys(cf.dtype, cf.head_dim);
-  int64_t key_tiles = 0;
   for (int r = 0; r < n_reqs; r++) {
     lens[r] = {reqs[r].n_cached, reqs[r].n_new};
     const int64_t tokens = (int64_t)reqs[r].n_cached + reqs[r].n_new;
     w->longest = std::max(w->longest, tokens);
     table_words += (tokens + kBlockTokens - 1) / kBlockTokens + 1;
-    key_tiles += (tokens + tile_keys - 1) / tile_keys;
     if (tokens > 0) rows_used.push_back(reqs[r].mass_row);
   }
-  if (key_tiles * cf.n_kv_heads > INT32_MAX) return fail(CALVO_EINVAL, "too many tokens in the batch");
-  w->key_tiles = (int)key_tiles;
   std::sort(rows_used.begin(), rows_used.end());
   w->mass_rows_differ = std::adjacent_find(rows_used.begin(), rows_used.end()) == rows_used.end() && (rows_used.empty() || rows_used.front() >= 0);
   w->max_mass_row = rows_used.empty() ? -1 : rows_used.back();
 
-  plan_window(cf.dtype == CALVO_F32, cf.head_dim, cf.n_q_heads / cf.n_kv_heads, cf.n_kv_heads, c->n_cus, lens, window, n_first, c->force_splits,
-              c->force_rows_tile, w->plan);
+  const char* forced = getenv("CALVO_ATTN_VARIANT");
+  const int variant = forced && forced[0] >= '3' && forced[0] <= '5' && forced[1] == 0 ? forced[0] - '0' : 0;
+  plan_window({cf.dtype == CALVO_F32, cf.head_dim, cf.n_q_heads, cf.n_kv_heads, c->n_cus, c->force_splits, c->force_rows_tile, variant}, lens, window,
+              n_first, w->plan);
+  const int tile_keys = attn_mass_tile_keys(cf.dtype, cf.head_dim);
+  plan_mass(cf.n_q_heads / cf.n_kv_heads, cf.n_kv_heads, c->n_cus, tile_keys, lens, window, n_first, w->mass);
+  const size_t n_mass = w->mass.items.size();
+  if ((int64_t)n_mass * cf.n_kv_heads > INT32_MAX) return fail(CALVO_EINVAL, "too many tokens in the batch");
+  const bool rows = w->plan.variant == kWindowRows;
   const size_t n_items = w->plan.items.size();
-  if ((int64_t)n_items * cf.n_kv_heads > INT32_MAX) return fail(CALVO_EINVAL, "too many new tokens");
+  if ((int64_t)n_items * cf.n_q_heads > INT32_MAX) return fail(CALVO_EINVAL, "too many new tokens");
 
-  // ---- words: work items, first items of cut tiles, requests, requests as the append launch takes them, tables
-  constexpr size_t kItem = sizeof(WinItem) / 4, kReq = sizeof(WinReq) / 4, kApp = sizeof(ReqDesc) / 4;
+  // ---- words: work items, first items of cut tiles, the same of the gathered weights, requests for the append, tables; pipelined kernels: the blocks'
+  // offsets in a layer, even blocks first, padded as in the causal batches (kTablePad)
+  constexpr size_t kItem = sizeof(WinItem) / 4, kMass = sizeof(MassItem) / 4, kAdd = sizeof(MassAdd) / 4, kApp = sizeof(ReqDesc) / 4;
   auto pad4 = [](size_t n) { return (n + 3) / 4 * 4; };
   w->items_at = 0;
   w->split_at = n_items * kItem;
-  w->reqs_at = pad4(w->split_at + w->plan.split_tiles.size());
-  w->append_at = w->reqs_at + (size_t)n_reqs * kReq;
+  w->mass_at = pad4(w->split_at + w->plan.split_tiles.size());
+  w->add_at = w->mass_at + n_mass * kMass;
+  w->append_at = w->add_at + w->mass.adds.size() * kAdd;
   w->tables_at = w->append_at + (size_t)n_reqs * kApp;
-  const size_t words = pad4(w->tables_at + (size_t)table_words);
-  const size_t pieces = w->plan.split_tiles.empty() ? 0 : n_items * (size_t)cf.n_kv_heads * (size_t)w->plan.shape.tile_rows;
+  w->offs_at = pad4(w->tables_at + (size_t)table_words);
+  auto offs_of = [](int64_t n_tab) { return n_tab + kTablePad + (n_tab & 1); };
+  size_t n_offs = 0;
+  for (int r = 0; r < n_reqs && !rows; r++) n_offs += (size_t)offs_of(((int64_t)reqs[r].n_cached + reqs[r].n_new + kBlockTokens - 1) / kBlockTokens);
+  const size_t words = pad4(w->offs_at + 2 * n_offs);
+  const size_t pieces = w->plan.split_tiles.empty() ? 0 : n_items * (size_t)w->plan.part_rows;
   w->part_o_at = (words + 63) / 64 * 64;
   w->part_ml_at = w->part_o_at + pieces * (size_t)w->plan.part_width;
-  if ((rc = take_buf(c, (w->part_ml_at + pieces * 2) * 4, words * 4, w->buf)) != CALVO_OK) return rc;
+  w->part_mass_at = w->part_ml_at + pieces * 2;
+  const size_t floats = w->part_mass_at + (size_t)w->mass.n_parts * (size_t)cf.n_kv_heads * (size_t)tile_keys;
+  if ((rc = take_buf(c, floats * 4, words * 4, w->buf)) != CALVO_OK) return rc;
 
   int32_t* h = w->buf.h;
-  std::vector<int32_t> table_off((size_t)n_reqs), q_off((size_t)n_reqs);
-  size_t at = 0;
-  int32_t q = 0, first_tile = 0;
+  std::vector<int32_t> table_off((size_t)n_reqs), mass_table((size_t)n_reqs), q_off((size_t)n_reqs);
+  int64_t* offs = (int64_t*)(h + w->offs_at);
+  size_t at = 0, offs_at = 0;
+  int32_t q = 0;
   for (int r = 0; r < n_reqs; r++) {
     const int64_t tokens = (int64_t)reqs[r].n_cached + reqs[r].n_new;
     const size_t n_tab = (size_t)((tokens + kBlockTokens - 1) / kBlockTokens);
-    table_off[r] = (int32_t)at;
+    table_off[r] = (int32_t)(rows ? at : offs_at);
+    mass_table[r] = (int32_t)at;
     q_off[r] = q;
+    if (!rows && n_tab) {
+      const size_t n = (size_t)offs_of((int64_t)n_tab);
+      for (size_t b = 0; b < n; b++)
+        offs[offs_at + (b & 1) * (n / 2) + b / 2] = (int64_t)reqs[r].block_table[std::min(b, n_tab - 1)] * (int64_t)c->blk_bytes;
+      offs_at += n;
+    }
     if (n_tab) memcpy(h + w->tables_at + at, reqs[r].block_table, n_tab * 4);
     h[w->tables_at + at + n_tab] = n_tab ? reqs[r].block_table[n_tab - 1] : 0;
-    const WinReq d = {(int32_t)at, reqs[r].n_cached, reqs[r].n_new, q, reqs[r].mass_row, first_tile, {0, 0}};
-    memcpy(h + w->reqs_at + (size_t)r * kReq, &d, sizeof d);
     const ReqDesc a = {(int32_t)at, reqs[r].n_cached, reqs[r].n_new, q};
     memcpy(h + w->append_at + (size_t)r * kApp, &a, sizeof a);
     at += n_tab + 1;
     q += reqs[r].n_new;
-    first_tile += (int32_t)((tokens + tile_keys - 1) / tile_keys);
   }
   for (size_t i = 0; i < n_items; i++) {
     const WindowPiece& x = w->plan.items[i];
     const WinItem d = {x.tile, x.sub_begin, x.sub_end, x.n_splits, x.first_item, table_off[x.req], reqs[x.req].n_cached, reqs[x.req].n_new,
-                       q_off[x.req], x.first_subs, x.gap, {0, 0, 0, 0, 0}};
+                       q_off[x.req], x.keys.first_subs, x.keys.gap, x.keys.n_full, x.keys.n_part, x.keys.edge, x.keys.n_edge, x.keys.diag};
     memcpy(h + i * kItem, &d, sizeof d);
+  }
+  for (size_t i = 0; i < n_mass; i++) {
+    const MassPiece& x = w->mass.items[i];
+    const MassItem d = {mass_table[x.req], reqs[x.req].n_cached, reqs[x.req].n_new, q_off[x.req], reqs[x.req].mass_row, x.tile, x.begin, x.end, x.part, {0, 0, 0}};
+    memcpy(h + w->mass_at + i * kMass, &d, sizeof d);
+  }
+  for (size_t i = 0; i < w->mass.adds.size(); i++) {
+    const MassTile& x = w->mass.adds[i];
+    const MassAdd d = {reqs[x.req].n_cached, reqs[x.req].n_cached + reqs[x.req].n_new, reqs[x.req].mass_row, x.tile, x.part, x.n_parts, {0, 0}};
+    memcpy(h + w->add_at + i * kAdd, &d, sizeof d);
   }
   if (!w->plan.split_tiles.empty()) memcpy(h + w->split_at, w->plan.split_tiles.data(), w->plan.split_tiles.size() * 4);
   return upload(c, w->buf, words);
@@ -317,13 +343,20 @@ int window_attn(calvo_window* w, int layer, const void* q, const void* k_new, co
   WinParams p{};
   p.q = q; p.out = out; p.lse = lse; p.pool_layer = pool_layer;
   p.items = (const WinItem*)(d + w->items_at); p.tables = d + w->tables_at;
+  p.blk_offs = (const int64_t*)(d + w->offs_at);
   p.n_q_heads = cf.n_q_heads; p.n_kv_heads = cf.n_kv_heads; p.head_dim = cf.head_dim;
   p.group = (uint32_t)(cf.n_q_heads / cf.n_kv_heads);
   p.window = w->window; p.n_first = w->n_first;
   p.scale = scale_of(c, scale);
   p.part_o = (float*)d + w->part_o_at; p.part_ml = (float*)d + w->part_ml_at;
-  HIP_TRY(launch_attn_window(p, cf.dtype, w->plan.shape.tile_rows, (int)w->plan.items.size(), d + w->split_at, (int)w->plan.split_tiles.size(),
-                             c->s_compute));
+  const int n_items = (int)w->plan.items.size(), n_cut = (int)w->plan.split_tiles.size();
+  if (w->plan.variant == kWindowRows) {
+    HIP_TRY(launch_attn_window(p, cf.dtype, w->plan.tile_rows, n_items, d + w->split_at, n_cut, c->s_compute));
+  } else {
+    p.heads_per_wg = w->plan.heads_per_wg;
+    p.row_blocks_per_wg = attn_mfma_row_blocks(w->plan.variant);
+    HIP_TRY(launch_attn_window_pipe(p, w->plan.variant, n_items, d + w->split_at, n_cut, c->s_compute));
+  }
   return CALVO_OK;
 }
 
@@ -333,8 +366,9 @@ int attn_mass(calvo_window* w, int layer, const void* q, const float* lse, const
   const calvo_config& cf = c->cfg;
   int rc = check_layer(c, layer);
   if (rc != CALVO_OK) return rc;
+  if (cf.n_q_heads / cf.n_kv_heads > 4096) return fail(CALVO_EINVAL, "more than 4096 query heads to a KV head");
   if (mass_rows < 0 || last_rows < 0) return fail(CALVO_EINVAL, "mass_rows and last_rows must not be negative");
-  if (w->key_tiles > 0) {
+  if (!w->mass.items.empty()) {
     if (!mass_out) return fail(CALVO_EINVAL, "mass_out is NULL");
     if (w->total > 0 && (!q || !lse)) return fail(CALVO_EINVAL, "q or lse is NULL");
     if (((uintptr_t)q & 15) != 0) return fail(CALVO_EINVAL, "q must be 16-byte aligned");
@@ -356,13 +390,14 @@ int attn_mass(calvo_window* w, int layer, const void* q, const float* lse, const
   MassParams p{};
   p.q = q; p.lse = lse; p.mass_in = mass_in; p.mass_out = mass_out;
   p.pool_layer = (const unsigned char*)cf.pool + (int64_t)layer * c->layer_bytes;
-  p.reqs = (const WinReq*)(w->buf.d + w->reqs_at); p.tables = w->buf.d + w->tables_at;
-  p.mass_stride = mass_stride; p.n_reqs = w->n_reqs; p.n_tiles = w->key_tiles;
+  p.items = (const MassItem*)(w->buf.d + w->mass_at); p.tables = w->buf.d + w->tables_at;
+  p.part = (float*)w->buf.d + w->part_mass_at;
+  p.mass_stride = mass_stride; p.n_items = (int32_t)w->mass.items.size();
   p.n_q_heads = cf.n_q_heads; p.n_kv_heads = cf.n_kv_heads; p.head_dim = cf.head_dim;
   p.group = (uint32_t)(cf.n_q_heads / cf.n_kv_heads);
   p.window = w->window; p.n_first = w->n_first; p.last_rows = last_rows;
   p.scale = scale_of(c, scale);
-  HIP_TRY(launch_attn_mass(p, cf.dtype, c->s_compute));
+  HIP_TRY(launch_attn_mass(p, cf.dtype, (const MassAdd*)(w->buf.d + w->add_at), (int)w->mass.adds.size(), c->s_compute));
   return CALVO_OK;
 }
 

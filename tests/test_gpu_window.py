@@ -44,6 +44,27 @@ def test_long_context(dim):
     run_and_check(Case([(6007, 1)], 16, 2, dim, seed=4, layers=2), FULL, 0)
 
 
+# CALVO_ATTN_VARIANT: 64 or 32 query rows per wave in the pipelined kernels, 5 the packed rows
+@pytest.mark.parametrize("variant", ["3", "4", "5"])
+@pytest.mark.parametrize("hq,hkv", [(8, 2), (32, 8), (5, 1), (4, 2)])
+@pytest.mark.parametrize("pieces", ["0", "2", "7"])
+def test_kernels_of_128_wide_heads(variant, hq, hkv, pieces, monkeypatch):
+    monkeypatch.setenv("CALVO_ATTN_VARIANT", variant)
+    if pieces != "0":
+        monkeypatch.setenv("CALVO_ATTN_SPLITS", pieces)
+    for window, n_first in WINDOWS:
+        for i, lens in enumerate([[(0, 1), (17, 3)], [(100, 1), (0, 33), (257, 70), (31, 2)], [(433, 130), (1200, 65)]]):
+            run_and_check(Case(lens, hq, hkv, 128, seed=300 + i), window, n_first)
+
+
+@pytest.mark.parametrize("variant", ["3", "4", "5"])
+def test_long_contexts_of_128_wide_heads(variant, monkeypatch):
+    """The steady loop with and without whole sub-tiles of first tokens in front."""
+    monkeypatch.setenv("CALVO_ATTN_VARIANT", variant)
+    for window, n_first in [(1000, 0), (1300, 300), (777, 1), (FULL, 0)]:
+        run_and_check(Case([(6007, 40), (2048, 2)], 8, 2, 128, seed=31), window, n_first)
+
+
 def test_scale():
     c = Case([(50, 20)], seed=5)
     wh.check_attn(c, c.run(30, 2, scale=0.5), 30, 2, scale=0.5)
@@ -52,10 +73,14 @@ def test_scale():
 @pytest.mark.parametrize("dtype,hq,hkv,dim", [("bf16", 8, 2, 128), ("bf16", 6, 2, 64), ("bf16", 4, 1, 256), ("f32", 6, 3, 64), ("f32", 4, 2, 128)])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("pieces", ["0", "3"])
-def test_hidden_keys_do_not_reach_a_row(dtype, hq, hkv, dim, value, pieces, monkeypatch):
+@pytest.mark.parametrize("variant", ["3", "4", "5"])
+def test_hidden_keys_do_not_reach_a_row(dtype, hq, hkv, dim, value, pieces, variant, monkeypatch):
     """K and V of cached tokens and of new ones hold `value`: rows that do not see them are within the bounds of a pool without.  (Not its
     bits: how far a row's softmax reference lies above its maximum depends on the rows beside it.)"""
+    if variant != "5" and (dtype, dim) != ("bf16", 128):
+        pytest.skip("one kernel only")
     monkeypatch.setenv("CALVO_ATTN_SPLITS", pieces)
+    monkeypatch.setenv("CALVO_ATTN_VARIANT", variant)
     c = Case([(150, 90)], hq, hkv, dim, dtype, seed=11)
     window, n_first, poisoned = 40, 5, [3, 30, 120, 149, 150 + 20, 150 + 61]
     t = c.tables[0]
