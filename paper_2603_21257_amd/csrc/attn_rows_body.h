@@ -453,6 +453,30 @@ __global__ void __launch_bounds__(64 * C::NW) attn_rows_kernel(typename C::Param
     }
   };
 
+  // WIN, every request a single tile: the wave that meets a step with new tokens stores their K and V first.  Nobody else reads these lines before
+  // (a head's row is whole lines), so the L1 holds nothing older; the step itself comes behind the wait.
+  if constexpr (WIN) {
+    if (p.k_new) {
+      const int cpr = D * E / 16, first_new = P / (kBlockTokens * KB) - gap;
+      int s = st_begin + (max(0, first_new - st_begin) + NW - 1) / NW * NW;
+      if (s < st_end) {
+        for (; s < st_end; s += NW) {
+          const int k0 = step_at(s) * (kBlockTokens * KB), from = max(P, k0), n = (min(ctx_len, k0 + kBlockTokens * KB) - from) * cpr;
+          for (int i = lane; i < n; i += 64) {
+            const int row = i / cpr, pos = from + row;
+            const unsigned in_row = head_b + 16 * (i - row * cpr);
+            const int64_t src = (int64_t)(rd.q_off + pos - P) * rs + in_row;
+            unsigned char* dst = const_cast<unsigned char*>(pool) + (uint64_t)(unsigned)p.tables[rd.table_off + pos / kBlockTokens] * (2 * half) + (pos % kBlockTokens) * rs + in_row;
+            const u32x4 k = *(const u32x4*)((const unsigned char*)p.k_new + src), v = *(const u32x4*)((const unsigned char*)p.v_new + src);
+            *(u32x4*)dst = k;
+            *(u32x4*)(dst + half) = v;
+          }
+        }
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+      }
+    }
+  }
+
   if (st < st_end) {
     // Requested Q, K, V, as in the loop, and Q waited for before it: a wait for K is then a wait for all but the V requests behind
     // it.  (Left to the scheduler, or with a test around the requests of a step, every step waited for the V it had just asked for.)

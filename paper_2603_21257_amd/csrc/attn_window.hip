@@ -16,17 +16,23 @@ hipError_t launch_window(const WinParams& p, unsigned grid, const int32_t* split
   return hipGetLastError();
 }
 
-// f(configuration) for an element type, head width and tiling (attn_rows_shape)
+// f(configuration) for an element type, head width and tiling: those of the causal launches (attn_rows_shape), and up to 128-wide heads one
+// block of 16 rows for single tokens (window_plan.cpp)
 template <typename F>
 auto with_window_cfg(int dtype, int head_dim, int tile_rows, F&& f) {
   typedef uint16_t B16;
   if (dtype == CALVO_F32) {
-    if (head_dim == 64) return f(WinRowsCfg<float, 64, 2, 2, 8, true>{});
-    if (head_dim < 64) return f(WinRowsCfg<float, 64, 2, 2, 8, false>{});
-    if (head_dim == 128) return f(WinRowsCfg<float, 128, 2, 1, 4, true>{});
-    if (head_dim < 128) return f(WinRowsCfg<float, 128, 2, 1, 4, false>{});
+    if (head_dim == 64) return tile_rows == 16 ? f(WinRowsCfg<float, 64, 1, 2, 8, true>{}) : f(WinRowsCfg<float, 64, 2, 2, 8, true>{});
+    if (head_dim < 64) return tile_rows == 16 ? f(WinRowsCfg<float, 64, 1, 2, 8, false>{}) : f(WinRowsCfg<float, 64, 2, 2, 8, false>{});
+    if (head_dim == 128) return tile_rows == 16 ? f(WinRowsCfg<float, 128, 1, 1, 8, true>{}) : f(WinRowsCfg<float, 128, 2, 1, 4, true>{});
+    if (head_dim < 128) return tile_rows == 16 ? f(WinRowsCfg<float, 128, 1, 1, 8, false>{}) : f(WinRowsCfg<float, 128, 2, 1, 4, false>{});
     if (head_dim == 256) return tile_rows == 32 ? f(WinRowsCfg<float, 256, 2, 1, 4, true>{}) : f(WinRowsCfg<float, 256, 1, 1, 4, true>{});
     return tile_rows == 32 ? f(WinRowsCfg<float, 256, 2, 1, 4, false>{}) : f(WinRowsCfg<float, 256, 1, 1, 4, false>{});
+  }
+  if (tile_rows == 16 && head_dim <= 128) {
+    if (head_dim == 64) return f(WinRowsCfg<B16, 64, 1, 2, 8, true>{});
+    if (head_dim < 64) return f(WinRowsCfg<B16, 64, 1, 2, 8, false>{});
+    return head_dim == 128 ? f(WinRowsCfg<B16, 128, 1, 2, 8, true>{}) : f(WinRowsCfg<B16, 128, 1, 2, 8, false>{});
   }
   if (head_dim == 64) return tile_rows == 64 ? f(WinRowsCfg<B16, 64, 4, 2, 8, true>{}) : f(WinRowsCfg<B16, 64, 2, 2, 8, true>{});
   if (head_dim < 64) return tile_rows == 64 ? f(WinRowsCfg<B16, 64, 4, 2, 8, false>{}) : f(WinRowsCfg<B16, 64, 2, 2, 8, false>{});

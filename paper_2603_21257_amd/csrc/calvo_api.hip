@@ -18,6 +18,7 @@
 
 #include "calvo_ctx.h"
 #include "ingest_plan.h"
+#include "window_plan.h"
 
 using namespace calvo;
 using namespace calvo::host;
@@ -348,6 +349,7 @@ int window_kernels_ready(calvo_ctx* c) {
   HIP_TRY(attn_window_prepare(c->cfg.dtype, c->cfg.head_dim, attn_rows_shape(f32, c->cfg.head_dim, false).tile_rows));
   if (attn_rows_has_large(f32, c->cfg.head_dim))
     HIP_TRY(attn_window_prepare(c->cfg.dtype, c->cfg.head_dim, attn_rows_shape(f32, c->cfg.head_dim, true).tile_rows));
+  if (c->cfg.head_dim <= 128) HIP_TRY(attn_window_prepare(c->cfg.dtype, c->cfg.head_dim, kFewRows));
   if (!f32 && c->cfg.head_dim == 128) HIP_TRY(attn_window_pipe_prepare());
   c->window_kernels = true;
   return CALVO_OK;

@@ -139,6 +139,8 @@ struct WinParams {
   const void* q;
   void* out;
   float* lse;                // or NULL: log-sum-exp of every row, [tokens][query heads]
+  const void* k_new;         // packed rows, where every request is a single tile: the launch stores these rows to the pool itself; else NULL
+  const void* v_new;
   void* pool_layer;
   const WinItem* items;
   const int32_t* tables;     // packed rows: what table_off of an item counts in ...
@@ -206,7 +208,7 @@ struct EvictParams {
   int64_t layer_bytes, mass_layer, mass_stride, out_layer, out_stride, kept_stride;
   int32_t n_reqs, n_layers, n_kv_heads;
   int32_t row_chunks;        // 16-byte chunks of one head's K (or V) of a token
-  int32_t max_keep;          // most tokens that a request keeps
+  int32_t max_tokens, max_keep;   // most tokens that a request has and keeps
 };
 hipError_t launch_evict_select(const EvictParams& p, hipStream_t stream);
 hipError_t launch_evict_move(const EvictParams& p, hipStream_t stream);

@@ -58,16 +58,26 @@ bool capturing(calvo_ctx* c) {
 }
 
 // ---- descriptor buffers.  One that is given back is used again behind the launches that read it, on the same stream, so nobody waits for
-// them; only its pinned source must have been read before it is written again.
+// them; only its pinned source must have been read before it is written again.  A few are kept in turn, so that a program that is some steps
+// ahead of the device finds one that has been.
 int take_buf(calvo_ctx* c, size_t d_bytes, size_t h_bytes, StepBuf& out) {
+  constexpr int kInTurn = 4;
   {
     std::lock_guard<std::mutex> lk(c->blob_mu);
-    int best = -1;
+    int best = -1, fit = 0;
+    bool best_read = false;
     for (int i = 0; i < (int)c->step_free.size(); i++) {
-      const StepBuf& b = c->step_free[i];
-      if (b.d_bytes >= d_bytes && b.h_bytes >= h_bytes && (best < 0 || b.d_bytes < c->step_free[best].d_bytes)) best = i;
+      StepBuf& b = c->step_free[i];
+      if (b.d_bytes < d_bytes || b.h_bytes < h_bytes) continue;
+      fit++;
+      if (b.pending && !best_read) {
+        if (hipEventQuery(b.read) == hipSuccess) b.pending = false;
+        else (void)hipGetLastError();
+      }
+      const bool better = best < 0 || (!b.pending && !best_read) || (!b.pending && b.d_bytes < c->step_free[best].d_bytes);
+      if (better) { best = i; best_read = !b.pending; }
     }
-    if (best >= 0) {
+    if (best >= 0 && (best_read || fit >= kInTurn)) {
       out = c->step_free[best];
       c->step_free.erase(c->step_free.begin() + best);
     }
@@ -332,7 +342,10 @@ int window_attn(calvo_window* w, int layer, const void* q, const void* k_new, co
   if ((rc = queue_behind_layer(c, layer)) != CALVO_OK) return rc;
   if (w->total == 0) return CALVO_OK;
   const int32_t* d = w->buf.d;
-  if (k_new) {
+  // The attention launch stores the new rows itself where every request is one tile of packed rows (decoding) and a head's row is whole cache
+  // lines: one launch less.
+  const bool along = k_new && w->plan.single_tiles && (size_t)cf.head_dim * c->elt % 128 == 0;
+  if (k_new && !along) {
     AppendParams app{};
     app.k_suffix = k_new; app.v_suffix = v_new; app.pool_layer = pool_layer;
     app.reqs = (const ReqDesc*)(d + w->append_at); app.tables = d + w->tables_at;
@@ -342,6 +355,7 @@ int window_attn(calvo_window* w, int layer, const void* q, const void* k_new, co
   }
   WinParams p{};
   p.q = q; p.out = out; p.lse = lse; p.pool_layer = pool_layer;
+  if (along) { p.k_new = k_new; p.v_new = v_new; }
   p.items = (const WinItem*)(d + w->items_at); p.tables = d + w->tables_at;
   p.blk_offs = (const int64_t*)(d + w->offs_at);
   p.n_q_heads = cf.n_q_heads; p.n_kv_heads = cf.n_kv_heads; p.head_dim = cf.head_dim;
@@ -501,6 +515,7 @@ int kv_evict(calvo_ctx* c, const calvo_evict_request* reqs, int n_reqs, int laye
     p.kept_stride = kept_stride;
     p.n_reqs = n_reqs; p.n_layers = n_layers; p.n_kv_heads = cf.n_kv_heads;
     p.row_chunks = (int32_t)((size_t)cf.head_dim * c->elt / 16);
+    p.max_tokens = (int32_t)longest;
     p.max_keep = max_keep;
     hipError_t e = launch_evict_select(p, c->s_compute);
     if (e == hipSuccess) e = launch_evict_move(p, c->s_compute);

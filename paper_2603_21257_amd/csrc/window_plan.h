@@ -33,10 +33,13 @@ struct WindowPlan {
   int variant = kWindowRows;
   int tile_rows = 0;                     // packed rows: the tiling
   int heads_per_wg = 1;                  // pipelined
+  bool single_tiles = false;             // packed rows: no request has more than one tile
   int64_t part_rows = 0, part_width = 0; // rows of partial results that a work item leaves over all heads, floats of one
   std::vector<WindowPiece> items;
   std::vector<int32_t> split_tiles;      // first item of every cut tile
 };
+
+constexpr int kFewRows = 16;             // tile_rows for single tokens
 
 struct WindowShape {
   bool f32;
