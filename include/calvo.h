@@ -42,7 +42,8 @@
  * workgroups of the zero-copy scatter; CALVO_MERGE_MIB = most bytes of
  * consecutive small layers that one transfer carries (default 256, 0 = every
  * layer by itself).  Read by every calvo_prefill_attn:
- * CALVO_ATTN_VARIANT = 3 or 4 forces the bf16 kernel with 64 or with 32 query rows per wave.
+ * CALVO_ATTN_VARIANT = 3 or 4 forces the bf16 kernel with 64 or with 32 query rows per wave; read by
+ * calvo_window_prepare as well, where 5 forces the packed-rows kernel.
  * Test hooks, read by calvo_create: CALVO_INGEST_DELAY_US = n makes the host
  * sleep n microseconds before it queues each transfer of the L2 -> L1 stage
  * (the loading stage becomes the slow one; nothing on the device changes);
@@ -352,6 +353,18 @@ typedef struct {
  * than 65535 requests or layers; CALVO_ENOMEM if a request needs more slots than the pool has or a buffer cannot be had. */
 int calvo_kv_evict(calvo_ctx* ctx, const calvo_evict_request* reqs, int n_reqs, int layer_begin, int layer_end, const float* mass, int32_t mass_rows,
                    int64_t mass_stride, int32_t* kept, int64_t kept_stride, float* mass_out, int64_t out_stride);
+
+/* Planning helper (host code, needs no GPU; cfg->pool is not looked at): the checks of calvo_window_prepare, and what calvo_window_attn would launch on a
+ * device with n_cus compute units.  *kernel (may be NULL): 3 or 4 as in calvo_attn_kernel_info, -1 the packed-rows kernel.  entries: HOST array
+ * of 7 * capacity int32, filled with runs of 32-key sub-tiles that a work item meets: (request, first row, end row, first sub-tile,
+ * end sub-tile, 1 if the kernel takes it that every row sees all of their keys, pieces of the tile), rows = (token, query head of a KV head) pairs
+ * of the request, token-major; *n_entries: their number.  CALVO_ENOMEM if capacity is too small (*n_entries is set), CALVO_EINVAL as
+ * calvo_window_prepare. */
+int calvo_window_plan(const calvo_config* cfg, int32_t n_cus, const calvo_window_request* reqs, int32_t n_reqs, int32_t window, int32_t n_first,
+                      int32_t* kernel, int32_t* entries, int32_t capacity, int32_t* n_entries);
+
+/* The checks that calvo_kv_evict makes of its requests (host code, needs no GPU; cfg->pool is not looked at). */
+int calvo_evict_check(const calvo_config* cfg, const calvo_evict_request* reqs, int32_t n_reqs, int32_t mass_rows);
 
 /* ---- Inter-request scheduling (paper Section 3.2; compared policies: Section 4.3).  Host code only.
  *

@@ -24,7 +24,8 @@ CALVO_EV_QUERY, CALVO_EV_HOST_WAIT, CALVO_EV_STREAM_WAIT = 0, 1, 2
 LIB_PATH = os.environ.get("CALVO_LIB") or os.path.join(os.path.dirname(os.path.abspath(__file__)), "libcalvo.so")
 EXPORTS = ["calvo_create", "calvo_destroy", "calvo_kv_ingest", "calvo_kv_ingest_chunked", "calvo_chunk_count",
            "calvo_chunk_event", "calvo_kv_ingest_l3", "calvo_l3_wait", "calvo_layer_event", "calvo_prefill_attn", "calvo_prefill_attn_noalloc", "calvo_batch_prepare", "calvo_batch_destroy", "calvo_prefill_attn_batch",
-           "calvo_window_prepare", "calvo_window_destroy", "calvo_window_attn", "calvo_attn_mass", "calvo_kv_evict", "calvo_attn_kernel_ms", "calvo_mfma_peak", "calvo_attn_kernel_info", "calvo_attn_tile_rows", "calvo_attn_plan", "calvo_attn_plan_items", "calvo_ingest_plan", "calvo_cost_fit", "calvo_cost_estimate",
+           "calvo_window_prepare", "calvo_window_destroy", "calvo_window_attn", "calvo_attn_mass", "calvo_kv_evict",
+           "calvo_window_plan", "calvo_evict_check", "calvo_attn_kernel_ms", "calvo_mfma_peak", "calvo_attn_kernel_info", "calvo_attn_tile_rows", "calvo_attn_plan", "calvo_attn_plan_items", "calvo_ingest_plan", "calvo_cost_fit", "calvo_cost_estimate",
            "calvo_sched_pick", "calvo_sched_simulate", "calvo_pool_create", "calvo_pool_destroy", "calvo_pool_reserve",
            "calvo_pool_retain", "calvo_pool_release", "calvo_pool_counts", "calvo_pool_admit", "calvo_pool_retry",
            "calvo_pool_cancel", "calvo_dispatch_create", "calvo_dispatch_submit", "calvo_dispatch_wait", "calvo_dispatch_poll",
@@ -141,6 +142,9 @@ def lib() -> C.CDLL:
                                       C.c_float]
         L.calvo_kv_evict.argtypes = [C.c_void_p, C.POINTER(calvo_evict_request), C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int32, C.c_int64,
                                      C.c_void_p, C.c_int64, C.c_void_p, C.c_int64]
+        L.calvo_window_plan.argtypes = [C.POINTER(calvo_config), C.c_int32, C.POINTER(calvo_window_request), C.c_int32, C.c_int32, C.c_int32,
+                                        C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int32, C.POINTER(C.c_int32)]
+        L.calvo_evict_check.argtypes = [C.POINTER(calvo_config), C.POINTER(calvo_evict_request), C.c_int32, C.c_int32]
         L.calvo_mfma_peak.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_double)]
         L.calvo_attn_kernel_ms.argtypes = [C.c_void_p, C.c_int, C.POINTER(C.c_float)]
         L.calvo_attn_plan.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int32,
@@ -381,6 +385,30 @@ def calvo_kv_evict(ctx: int, reqs: Sequence[calvo_evict_request], layer_begin: i
                    kept, kept_stride: int, mass_out=None, out_stride: int = 0) -> None:
     _check(lib().calvo_kv_evict(ctx, _struct_array(calvo_evict_request, reqs), len(reqs), layer_begin, layer_end, _ptr(mass), int(mass_rows),
                                 int(mass_stride), _ptr(kept), int(kept_stride), _ptr(mass_out), int(out_stride)))
+
+
+def _shape_config(n_q_heads, n_kv_heads, head_dim, dtype, pool_blocks) -> calvo_config:
+    return calvo_config(1, n_q_heads, n_kv_heads, head_dim, 16, dtype, pool_blocks, None, 0, 0, 0, None)
+
+
+def calvo_window_plan(n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int, pool_blocks: int, n_cus: int, reqs, window: int,
+                      n_first: int = 0):
+    """(kernel id, int32 array [n][7] of runs of sub-tiles) that calvo_window_attn would launch; needs no GPU."""
+    cfg = _shape_config(n_q_heads, n_kv_heads, head_dim, dtype, pool_blocks)
+    arr, kernel, n = _struct_array(calvo_window_request, reqs), C.c_int32(), C.c_int32()
+    args = (C.byref(cfg), int(n_cus), arr, len(reqs), int(window), int(n_first), C.byref(kernel))
+    rc = lib().calvo_window_plan(*args, None, 0, C.byref(n))
+    if rc == CALVO_ENOMEM and n.value > 0:
+        out = np.zeros((n.value, 7), np.int32)
+        _check(lib().calvo_window_plan(*args, out.ctypes.data_as(C.POINTER(C.c_int32)), n.value, C.byref(n)))
+        return kernel.value, out
+    _check(rc)
+    return kernel.value, np.zeros((0, 7), np.int32)
+
+
+def calvo_evict_check(n_kv_heads: int, head_dim: int, dtype: int, pool_blocks: int, reqs, mass_rows: int) -> None:
+    cfg = _shape_config(n_kv_heads, n_kv_heads, head_dim, dtype, pool_blocks)
+    _check(lib().calvo_evict_check(C.byref(cfg), _struct_array(calvo_evict_request, reqs), len(reqs), int(mass_rows)))
 
 
 CALVO_MFMA_16x16x32, CALVO_MFMA_32x32x16 = 0, 1

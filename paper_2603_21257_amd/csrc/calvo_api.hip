@@ -131,6 +131,11 @@ void destroy_partial(calvo_ctx* c) {
   delete c;
 }
 
+}  // namespace
+
+namespace calvo {
+namespace host {
+
 int validate_config(const calvo_config* cfg) {
   if (!cfg) return fail(CALVO_EINVAL, "config is NULL");
   if (cfg->n_layers <= 0) return fail(CALVO_EINVAL, "n_layers must be positive");
@@ -153,11 +158,6 @@ int validate_config(const calvo_config* cfg) {
     return fail(CALVO_EINVAL, "staging_bytes (%zu) is smaller than one block (%zu)", cfg->staging_bytes, blk);
   return CALVO_OK;
 }
-
-}  // namespace
-
-namespace calvo {
-namespace host {
 
 // Checks shared by ingest and attention.  Nothing is queued before these pass.
 int validate_requests(const calvo_ctx* c, const calvo_request* reqs, int n_reqs, bool need_host,

@@ -23,6 +23,12 @@ struct StepBuf {
   hipEvent_t read = nullptr;
   bool pending = false;
 };
+
+// Per slot the mark of the last table check that met it (calvo_window.hip); a check takes marks that no slot carries, so that nothing is cleared
+struct SlotMarks {
+  std::vector<uint32_t> of;
+  uint32_t next = 1;
+};
 }  // namespace calvo
 
 struct calvo_ctx {
@@ -118,9 +124,7 @@ struct calvo_ctx {
   std::mutex blob_mu;
   std::vector<BlobBuf> blob_free;
   std::vector<calvo::StepBuf> step_free;      // of calvo_window.hip, given back (guarded by blob_mu)
-  // per slot: the mark of the last table check that met it (calvo_window.hip); a check takes marks that no slot carries
-  std::vector<uint32_t> slot_marks;
-  uint32_t next_mark = 1;
+  calvo::SlotMarks marks;
   bool window_kernels = false;               // their LDS limits are raised
   std::vector<void*> l2_ring;
   std::vector<hipEvent_t> ev_l2_free;
@@ -163,6 +167,9 @@ void parallel_copy(unsigned char* dst, const unsigned char* src, size_t n, int n
 // Queues the compute stream behind the layer's most recent load (with a running L3 loader after a wait for its hand-over).  While the
 // stream is captured nothing outside can be waited for: CALVO_ENOTREADY unless the layer is in.
 int queue_behind_layer(calvo_ctx* c, int layer);
+
+// shape, element type, pool and staging sizes of a configuration
+int validate_config(const calvo_config* cfg);
 
 // Raises the LDS limits of the window kernels for the context's shape, once
 int window_kernels_ready(calvo_ctx* c);

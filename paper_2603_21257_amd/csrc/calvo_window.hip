@@ -126,30 +126,31 @@ int upload(calvo_ctx* c, StepBuf& b, size_t words) {
   return CALVO_OK;
 }
 
-// Slots of a table, marked in c->slot_marks with `mark`; a slot that carries `mark` already is refused.  `other`, if not 0: another mark that
-// is refused as well.
-int mark_table(calvo_ctx* c, const int32_t* table, int64_t from, int64_t n, uint32_t mark, const char* what, int r) {
-  for (int64_t j = from; j < n; j++) {
+// Slots of a table get `mark`; one that has it already is refused.
+int mark_table(const calvo_config& cf, SlotMarks& marks, const int32_t* table, int64_t n, uint32_t mark, const char* what, int r) {
+  for (int64_t j = 0; j < n; j++) {
     const int32_t s = table[j];
-    if (s < 0 || s >= c->cfg.pool_blocks)
+    if (s < 0 || s >= cf.pool_blocks)
       return fail(CALVO_EINVAL, "request %d: slot %d at %s[%lld] is outside the pool (not allocated)", r, s, what, (long long)j);
-    if (c->slot_marks[s] == mark) return fail(CALVO_EINVAL, "request %d: slot %d appears twice in %s", r, s, what);
-    c->slot_marks[s] = mark;
+    if (marks.of[s] == mark) return fail(CALVO_EINVAL, "request %d: slot %d appears twice in %s", r, s, what);
+    marks.of[s] = mark;
   }
   return CALVO_OK;
 }
 
 // n marks that no slot carries; returns the first
-uint32_t new_marks(calvo_ctx* c, uint32_t n) {
-  if (c->slot_marks.empty()) c->slot_marks.assign((size_t)c->cfg.pool_blocks, 0);
-  if (c->next_mark > UINT32_MAX - n) {
-    std::fill(c->slot_marks.begin(), c->slot_marks.end(), 0);
-    c->next_mark = 1;
+uint32_t new_marks(const calvo_config& cf, SlotMarks& marks, uint32_t n) {
+  if (marks.of.empty()) marks.of.assign((size_t)cf.pool_blocks, 0);
+  if (marks.next > UINT32_MAX - n) {
+    std::fill(marks.of.begin(), marks.of.end(), 0);
+    marks.next = 1;
   }
-  const uint32_t first = c->next_mark;
-  c->next_mark += n;
+  const uint32_t first = marks.next;
+  marks.next += n;
   return first;
 }
+
+int64_t blocks_of(int64_t tokens) { return (tokens + kBlockTokens - 1) / kBlockTokens; }
 
 struct Range {
   uintptr_t at;
@@ -165,7 +166,10 @@ float scale_of(const calvo_ctx* c, float scale) { return scale > 0.f ? scale : 1
 
 constexpr int64_t kMostTokens = INT32_MAX - 65536;     // positions and their sums with tile sizes stay within 32 bits
 
-int check_window_requests(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, int64_t* total) {
+int check_window_requests(const calvo_config& cf, SlotMarks& marks, const calvo_window_request* reqs, int n_reqs, int32_t window, int32_t n_first,
+                          int64_t* total) {
+  if (window < 1) return fail(CALVO_EINVAL, "window must be positive");
+  if (n_first < 0) return fail(CALVO_EINVAL, "n_first must not be negative");
   if (n_reqs < 0) return fail(CALVO_EINVAL, "n_reqs is negative");
   if (n_reqs > 0 && !reqs) return fail(CALVO_EINVAL, "reqs is NULL");
   *total = 0;
@@ -174,45 +178,79 @@ int check_window_requests(calvo_ctx* c, const calvo_window_request* reqs, int n_
     if (q.n_cached < 0 || q.n_new < 0) return fail(CALVO_EINVAL, "request %d: negative token count", r);
     const int64_t tokens = (int64_t)q.n_cached + q.n_new;
     if (tokens > kMostTokens) return fail(CALVO_EINVAL, "request %d: context too long", r);
-    const int64_t n_tab = (tokens + kBlockTokens - 1) / kBlockTokens;
-    if (n_tab > c->cfg.pool_blocks)
-      return fail(CALVO_ENOMEM, "request %d needs %lld slots, the pool has %lld", r, (long long)n_tab, (long long)c->cfg.pool_blocks);
-    if (n_tab > 0 && !q.block_table) return fail(CALVO_EINVAL, "request %d: block_table is NULL", r);
+    if (blocks_of(tokens) > cf.pool_blocks)
+      return fail(CALVO_ENOMEM, "request %d needs %lld slots, the pool has %lld", r, (long long)blocks_of(tokens), (long long)cf.pool_blocks);
+    if (tokens > 0 && !q.block_table) return fail(CALVO_EINVAL, "request %d: block_table is NULL", r);
     if (q.reserved != 0) return fail(CALVO_EINVAL, "request %d: reserved must be 0", r);
     *total += q.n_new;
   }
-  if (*total * (c->cfg.n_q_heads / c->cfg.n_kv_heads) > INT32_MAX - 4096) return fail(CALVO_EINVAL, "too many new tokens");
+  if (*total * (cf.n_q_heads / cf.n_kv_heads) > INT32_MAX - 4096) return fail(CALVO_EINVAL, "too many new tokens");
   // every table by itself, then the slots that new tokens go to: they are in no other table
-  const uint32_t mark = new_marks(c, (uint32_t)n_reqs + 1), stored = mark + (uint32_t)n_reqs;
+  const uint32_t mark = new_marks(cf, marks, (uint32_t)n_reqs + 1), stored = mark + (uint32_t)n_reqs;
   for (int r = 0; r < n_reqs; r++) {
-    const int64_t n_tab = ((int64_t)reqs[r].n_cached + reqs[r].n_new + kBlockTokens - 1) / kBlockTokens;
-    const int rc = mark_table(c, reqs[r].block_table, 0, n_tab, mark + (uint32_t)r, "block_table", r);
+    const int rc = mark_table(cf, marks, reqs[r].block_table, blocks_of((int64_t)reqs[r].n_cached + reqs[r].n_new), mark + (uint32_t)r, "block_table", r);
     if (rc != CALVO_OK) return rc;
   }
-  if (n_reqs > 1) {
+  for (int pass = 0; pass < 2 && n_reqs > 1; pass++)
     for (int r = 0; r < n_reqs; r++) {
-      if (reqs[r].n_new == 0) continue;
-      const int64_t n_tab = ((int64_t)reqs[r].n_cached + reqs[r].n_new + kBlockTokens - 1) / kBlockTokens;
-      for (int64_t j = reqs[r].n_cached / kBlockTokens; j < n_tab; j++) {
-        uint32_t& m = c->slot_marks[reqs[r].block_table[j]];
+      const int64_t n_tab = blocks_of((int64_t)reqs[r].n_cached + reqs[r].n_new), own = reqs[r].n_new ? reqs[r].n_cached / kBlockTokens : n_tab;
+      // first the blocks that take new tokens, then those that are only read
+      for (int64_t j = pass ? 0 : own; j < (pass ? own : n_tab); j++) {
+        uint32_t& m = marks.of[reqs[r].block_table[j]];
         if (m == stored) return fail(CALVO_EINVAL, "request %d: slot %d takes new tokens of another request", r, reqs[r].block_table[j]);
-        m = stored;
+        if (!pass) m = stored;
       }
     }
-    for (int r = 0; r < n_reqs; r++) {
-      const int64_t n_tab = ((int64_t)reqs[r].n_cached + reqs[r].n_new + kBlockTokens - 1) / kBlockTokens;
-      const int64_t own = reqs[r].n_new ? reqs[r].n_cached / kBlockTokens : n_tab;
-      for (int64_t j = 0; j < own; j++)
-        if (c->slot_marks[reqs[r].block_table[j]] == stored)
-          return fail(CALVO_EINVAL, "request %d: slot %d takes new tokens of another request", r, reqs[r].block_table[j]);
-    }
-  }
   return CALVO_OK;
+}
+
+int check_evict_requests(const calvo_config& cf, SlotMarks& marks, const calvo_evict_request* reqs, int n_reqs, int32_t mass_rows) {
+  if (n_reqs < 0 || n_reqs > 65535) return fail(CALVO_EINVAL, "n_reqs outside [0, 65535]");
+  if (n_reqs > 0 && !reqs) return fail(CALVO_EINVAL, "reqs is NULL");
+  if (mass_rows < 0) return fail(CALVO_EINVAL, "mass_rows must not be negative");
+  std::vector<int32_t> used;
+  int64_t words = 0;
+  for (int r = 0; r < n_reqs; r++) {
+    const calvo_evict_request& q = reqs[r];
+    if (q.n_tokens < 0 || q.n_keep < 0 || q.n_first < 0 || q.n_last < 0) return fail(CALVO_EINVAL, "request %d: negative token count", r);
+    if (q.n_tokens > kMostTokens) return fail(CALVO_EINVAL, "request %d: context too long", r);
+    if (q.n_keep > q.n_tokens) return fail(CALVO_EINVAL, "request %d: keeps %d of %d tokens", r, q.n_keep, q.n_tokens);
+    if ((int64_t)q.n_first + q.n_last > q.n_keep) return fail(CALVO_EINVAL, "request %d: n_first + n_last is more than n_keep", r);
+    if (q.reserved != 0) return fail(CALVO_EINVAL, "request %d: reserved must be 0", r);
+    if (q.n_keep == 0) continue;
+    const int64_t slots = blocks_of(q.n_tokens) + blocks_of(q.n_keep);
+    if (slots > cf.pool_blocks)
+      return fail(CALVO_ENOMEM, "request %d needs %lld slots, the pool has %lld", r, (long long)slots, (long long)cf.pool_blocks);
+    if (!q.src_table || !q.dst_table) return fail(CALVO_EINVAL, "request %d: a table is NULL", r);
+    if (q.mass_row < 0 || q.mass_row >= mass_rows) return fail(CALVO_EINVAL, "request %d: mass_row %d outside [0, %d)", r, q.mass_row, mass_rows);
+    used.push_back(q.mass_row);
+    words += slots;
+  }
+  if (words > INT32_MAX) return fail(CALVO_EINVAL, "too many tokens in the call");
+  std::sort(used.begin(), used.end());
+  if (std::adjacent_find(used.begin(), used.end()) != used.end()) return fail(CALVO_EINVAL, "the requests' mass_row must differ");
+  // sources: distinct inside a request.  Destinations: distinct over the call, and no request's source.
+  const uint32_t mark = new_marks(cf, marks, (uint32_t)n_reqs + 1), dst = mark + (uint32_t)n_reqs;
+  int rc;
+  for (int r = 0; r < n_reqs; r++)
+    if (reqs[r].n_keep && (rc = mark_table(cf, marks, reqs[r].src_table, blocks_of(reqs[r].n_tokens), mark + (uint32_t)r, "src_table", r)) != CALVO_OK) return rc;
+  for (int r = 0; r < n_reqs; r++)
+    if (reqs[r].n_keep && (rc = mark_table(cf, marks, reqs[r].dst_table, blocks_of(reqs[r].n_keep), dst, "dst_table", r)) != CALVO_OK) return rc;
+  for (int r = 0; r < n_reqs; r++)
+    for (int64_t j = 0; reqs[r].n_keep && j < blocks_of(reqs[r].n_tokens); j++)
+      if (marks.of[reqs[r].src_table[j]] == dst) return fail(CALVO_EINVAL, "request %d: slot %d of src_table is in a dst_table", r, reqs[r].src_table[j]);
+  return CALVO_OK;
+}
+
+// CALVO_ATTN_VARIANT, read for every plan: 3 or 4 as for the causal kernels, 5 the packed rows
+int forced_variant() {
+  const char* e = getenv("CALVO_ATTN_VARIANT");
+  return e && e[0] >= '3' && e[0] <= '5' && e[1] == 0 ? e[0] - '0' : 0;
 }
 
 int window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, int32_t window, int32_t n_first, calvo_window* w) {
   int64_t total = 0;
-  int rc = check_window_requests(c, reqs, n_reqs, &total);
+  int rc = check_window_requests(c->cfg, c->marks, reqs, n_reqs, window, n_first, &total);
   if (rc != CALVO_OK) return rc;
   const calvo_config& cf = c->cfg;
   w->c = c; w->n_reqs = n_reqs; w->total = (int)total; w->window = window; w->n_first = n_first;
@@ -231,10 +269,8 @@ int window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, i
   w->mass_rows_differ = std::adjacent_find(rows_used.begin(), rows_used.end()) == rows_used.end() && (rows_used.empty() || rows_used.front() >= 0);
   w->max_mass_row = rows_used.empty() ? -1 : rows_used.back();
 
-  const char* forced = getenv("CALVO_ATTN_VARIANT");
-  const int variant = forced && forced[0] >= '3' && forced[0] <= '5' && forced[1] == 0 ? forced[0] - '0' : 0;
-  plan_window({cf.dtype == CALVO_F32, cf.head_dim, cf.n_q_heads, cf.n_kv_heads, c->n_cus, c->force_splits, c->force_rows_tile, variant}, lens, window,
-              n_first, w->plan);
+  plan_window({cf.dtype == CALVO_F32, cf.head_dim, cf.n_q_heads, cf.n_kv_heads, c->n_cus, c->force_splits, c->force_rows_tile, forced_variant()}, lens,
+              window, n_first, w->plan);
   const int tile_keys = attn_mass_tile_keys(cf.dtype, cf.head_dim);
   plan_mass(cf.n_q_heads / cf.n_kv_heads, cf.n_kv_heads, c->n_cus, tile_keys, lens, window, n_first, w->mass);
   const size_t n_mass = w->mass.items.size();
@@ -420,52 +456,18 @@ int kv_evict(calvo_ctx* c, const calvo_evict_request* reqs, int n_reqs, int laye
   const calvo_config& cf = c->cfg;
   if (layer_begin < 0 || layer_end > cf.n_layers || layer_begin > layer_end)
     return fail(CALVO_EINVAL, "layers [%d, %d) outside [0, %d)", layer_begin, layer_end, cf.n_layers);
-  if (n_reqs < 0 || n_reqs > 65535) return fail(CALVO_EINVAL, "n_reqs outside [0, 65535]");
-  if (n_reqs > 0 && !reqs) return fail(CALVO_EINVAL, "reqs is NULL");
   const int n_layers = layer_end - layer_begin;
   if (n_layers > 65535) return fail(CALVO_EINVAL, "more than 65535 layers");
-  if (mass_rows < 0) return fail(CALVO_EINVAL, "mass_rows must not be negative");
-  int64_t table_words = 0;
+  int rc = check_evict_requests(cf, c->marks, reqs, n_reqs, mass_rows);
+  if (rc != CALVO_OK) return rc;
+  int64_t table_words = 0, longest = 0;
   int32_t max_keep = 0;
-  int rc;
-  int64_t longest = 0;
-  std::vector<int32_t> used;
   for (int r = 0; r < n_reqs; r++) {
-    const calvo_evict_request& q = reqs[r];
-    if (q.n_tokens < 0 || q.n_keep < 0 || q.n_first < 0 || q.n_last < 0) return fail(CALVO_EINVAL, "request %d: negative token count", r);
-    if (q.n_tokens > kMostTokens) return fail(CALVO_EINVAL, "request %d: context too long", r);
-    if (q.n_keep > q.n_tokens) return fail(CALVO_EINVAL, "request %d: keeps %d of %d tokens", r, q.n_keep, q.n_tokens);
-    if ((int64_t)q.n_first + q.n_last > q.n_keep)
-      return fail(CALVO_EINVAL, "request %d: n_first + n_last is more than n_keep", r);
-    if (q.reserved != 0) return fail(CALVO_EINVAL, "request %d: reserved must be 0", r);
-    if (q.n_keep == 0) continue;
-    const int64_t ns = ((int64_t)q.n_tokens + kBlockTokens - 1) / kBlockTokens, nd = ((int64_t)q.n_keep + kBlockTokens - 1) / kBlockTokens;
-    if (ns + nd > cf.pool_blocks)
-      return fail(CALVO_ENOMEM, "request %d needs %lld slots, the pool has %lld", r, (long long)(ns + nd), (long long)cf.pool_blocks);
-    if (!q.src_table || !q.dst_table) return fail(CALVO_EINVAL, "request %d: a table is NULL", r);
-    if (q.mass_row < 0 || q.mass_row >= mass_rows) return fail(CALVO_EINVAL, "request %d: mass_row %d outside [0, %d)", r, q.mass_row, mass_rows);
-    used.push_back(q.mass_row);
-    table_words += ns + nd;
-    max_keep = std::max(max_keep, q.n_keep);
-    longest = std::max<int64_t>(longest, q.n_tokens);
+    if (reqs[r].n_keep == 0) continue;
+    table_words += blocks_of(reqs[r].n_tokens) + blocks_of(reqs[r].n_keep);
+    max_keep = std::max(max_keep, reqs[r].n_keep);
+    longest = std::max<int64_t>(longest, reqs[r].n_tokens);
   }
-  if (table_words > INT32_MAX) return fail(CALVO_EINVAL, "too many tokens in the call");
-  std::sort(used.begin(), used.end());
-  if (std::adjacent_find(used.begin(), used.end()) != used.end()) return fail(CALVO_EINVAL, "the requests' mass_row must differ");
-  // sources: distinct inside a request.  Destinations: distinct over the call, and no request's source.
-  const uint32_t mark = new_marks(c, (uint32_t)n_reqs + 1), dst_mark = mark + (uint32_t)n_reqs;
-  for (int r = 0; r < n_reqs; r++)
-    if (reqs[r].n_keep > 0 &&
-        (rc = mark_table(c, reqs[r].src_table, 0, ((int64_t)reqs[r].n_tokens + kBlockTokens - 1) / kBlockTokens, mark + (uint32_t)r, "src_table", r)) != CALVO_OK)
-      return rc;
-  for (int r = 0; r < n_reqs; r++)
-    if (reqs[r].n_keep > 0 &&
-        (rc = mark_table(c, reqs[r].dst_table, 0, ((int64_t)reqs[r].n_keep + kBlockTokens - 1) / kBlockTokens, dst_mark, "dst_table", r)) != CALVO_OK)
-      return rc;
-  for (int r = 0; r < n_reqs; r++)
-    for (int64_t j = 0; reqs[r].n_keep > 0 && j < ((int64_t)reqs[r].n_tokens + kBlockTokens - 1) / kBlockTokens; j++)
-      if (c->slot_marks[reqs[r].src_table[j]] == dst_mark)
-        return fail(CALVO_EINVAL, "request %d: slot %d of src_table is in a dst_table", r, reqs[r].src_table[j]);
   if (max_keep > 0 && n_layers > 0) {
     if (!mass || !kept) return fail(CALVO_EINVAL, "mass or kept is NULL");
     if ((((uintptr_t)mass | (uintptr_t)mass_out | (uintptr_t)kept) & 3) != 0) return fail(CALVO_EINVAL, "mass, mass_out and kept must be 4-byte aligned");
@@ -496,7 +498,7 @@ int kv_evict(calvo_ctx* c, const calvo_evict_request* reqs, int n_reqs, int laye
   int32_t* tables = buf.h + (size_t)n_reqs * kReq;
   for (int r = 0; r < n_reqs; r++) {
     const calvo_evict_request& q = reqs[r];
-    const int32_t ns = q.n_keep ? (q.n_tokens + kBlockTokens - 1) / kBlockTokens : 0, nd = (q.n_keep + kBlockTokens - 1) / kBlockTokens;
+    const int32_t ns = q.n_keep ? (int32_t)blocks_of(q.n_tokens) : 0, nd = (int32_t)blocks_of(q.n_keep);
     const EvictDesc d = {at, at + ns, q.n_keep ? q.n_tokens : 0, q.n_keep, q.n_first, q.n_last, q.n_keep ? q.mass_row : 0, 0};
     memcpy(buf.h + (size_t)r * kReq, &d, sizeof d);
     if (ns) memcpy(tables + at, q.src_table, (size_t)ns * 4);
@@ -533,8 +535,6 @@ int calvo_window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_r
   if (!out) return fail(CALVO_EINVAL, "out is NULL");
   *out = nullptr;
   if (!c) return fail(CALVO_EINVAL, "ctx is NULL");
-  if (window < 1) return fail(CALVO_EINVAL, "window must be positive");
-  if (n_first < 0) return fail(CALVO_EINVAL, "n_first must not be negative");
   calvo_window* w = new (std::nothrow) calvo_window();
   if (!w) return fail(CALVO_ENOMEM, "out of host memory");
   int rc = CALVO_OK;
@@ -561,6 +561,67 @@ int calvo_window_destroy(calvo_window* w) {
   }
   delete w;
   return CALVO_OK;
+}
+
+int calvo_window_plan(const calvo_config* cfg, int32_t n_cus, const calvo_window_request* reqs, int32_t n_reqs, int32_t window, int32_t n_first,
+                      int32_t* kernel, int32_t* entries, int32_t capacity, int32_t* n_entries) {
+  if (!cfg || n_cus <= 0 || capacity < 0 || (capacity > 0 && !entries) || !n_entries) return fail(CALVO_EINVAL, "bad argument");
+  calvo_config cf = *cfg;
+  cf.pool = (void*)16;                         // not looked at
+  int rc = validate_config(&cf);
+  if (rc != CALVO_OK) return rc;
+  try {
+    SlotMarks marks;
+    int64_t total = 0;
+    if ((rc = check_window_requests(cf, marks, reqs, n_reqs, window, n_first, &total)) != CALVO_OK) return rc;
+    std::vector<WindowLens> lens((size_t)n_reqs);
+    for (int r = 0; r < n_reqs; r++) lens[r] = {reqs[r].n_cached, reqs[r].n_new};
+    WindowPlan plan;
+    plan_window({cf.dtype == CALVO_F32, cf.head_dim, cf.n_q_heads, cf.n_kv_heads, n_cus, 0, 0, forced_variant()}, lens, window, n_first, plan);
+    if (kernel) *kernel = plan.variant;
+    int32_t n = 0;
+    const int group = cf.n_q_heads / cf.n_kv_heads;
+    for (const WindowPiece& x : plan.items) {
+      const int64_t rows = (int64_t)lens[(size_t)x.req].n_new * group, tr = plan.variant == kWindowRows ? plan.tile_rows : (int64_t)plan.tile_tokens * group;
+      // runs of the item's part of the list: where each begins in the list, how many, where in the context
+      const WindowKeys& k = x.keys;
+      const bool listed = plan.variant != kWindowRows;
+      const int32_t runs[5][3] = {{0, k.first_subs, 0},
+                                  {k.first_subs, listed ? k.n_full - k.first_subs : k.n - k.first_subs, k.first_subs + k.gap},
+                                  {k.n_full, listed ? k.n_part : 0, n_first / 32},
+                                  {k.n_full + k.n_part, listed ? k.n_edge : 0, k.edge},
+                                  {k.n_full + k.n_part + k.n_edge, listed ? k.n - k.n_full - k.n_part - k.n_edge : 0, k.diag}};
+      for (int i = 0; i < 5; i++) {
+        const int32_t b = std::max(x.sub_begin, runs[i][0]), e = std::min(x.sub_end, runs[i][0] + runs[i][1]);
+        if (b >= e) continue;
+        if (n < capacity) {
+          int32_t* o = entries + 7 * (int64_t)n;
+          o[0] = x.req; o[1] = (int32_t)(x.tile * tr); o[2] = (int32_t)std::min((x.tile + 1) * tr, rows);
+          o[3] = b - runs[i][0] + runs[i][2]; o[4] = e - runs[i][0] + runs[i][2];
+          o[5] = listed && i < 2; o[6] = x.n_splits;
+        }
+        n++;
+      }
+    }
+    *n_entries = n;
+    return n > capacity ? CALVO_ENOMEM : CALVO_OK;
+  } catch (const std::bad_alloc&) {
+    return fail(CALVO_ENOMEM, "out of host memory");
+  }
+}
+
+int calvo_evict_check(const calvo_config* cfg, const calvo_evict_request* reqs, int32_t n_reqs, int32_t mass_rows) {
+  if (!cfg) return fail(CALVO_EINVAL, "config is NULL");
+  calvo_config cf = *cfg;
+  cf.pool = (void*)16;
+  const int rc = validate_config(&cf);
+  if (rc != CALVO_OK) return rc;
+  try {
+    SlotMarks marks;
+    return check_evict_requests(cf, marks, reqs, n_reqs, mass_rows);
+  } catch (const std::bad_alloc&) {
+    return fail(CALVO_ENOMEM, "out of host memory");
+  }
 }
 
 int calvo_window_attn(calvo_window* w, int layer, const void* q, const void* k_new, const void* v_new, void* out, float* lse, float scale) {

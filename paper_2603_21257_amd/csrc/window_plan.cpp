@@ -130,6 +130,7 @@ void plan_window(const WindowShape& s, const std::vector<WindowLens>& lens, int3
     out.part_rows = (int64_t)s.n_kv_heads * best.shape.tile_rows;
     out.part_width = s.head_dim <= 64 ? 64 : s.head_dim <= 128 ? 128 : 256;
   } else {
+    out.tile_tokens = best.tile_tokens;
     out.part_rows = (int64_t)head_groups * attn_mfma_row_blocks(best.variant) * 32;
     out.part_width = 128;
   }

@@ -32,6 +32,7 @@ constexpr int kWindowRows = -1;          // the packed-rows kernel; else kAttnPi
 struct WindowPlan {
   int variant = kWindowRows;
   int tile_rows = 0;                     // packed rows: the tiling
+  int tile_tokens = 0;                   // pipelined: tokens of a tile
   int heads_per_wg = 1;                  // pipelined
   bool single_tiles = false;             // packed rows: no request has more than one tile
   int64_t part_rows = 0, part_width = 0; // rows of partial results that a work item leaves over all heads, floats of one

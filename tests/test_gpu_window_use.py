@@ -1,0 +1,348 @@
+"""The window operators together and as a program uses them: prompt, gathered weights, eviction and decoding over the pool's own allocator; plans in turn,
+captured graphs, streams, loads that are under way, and refusals of bad buffers."""
+import numpy as np
+import pytest
+import torch
+
+import window_harness as wh
+from oracle import window_oracle as wo
+from paper_2603_21257_amd import binding as cb
+from window_harness import FULL, U32, Case
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dim", [("bf16", 8, 2, 128), ("f32", 6, 3, 64), ("bf16", 4, 2, 40)])
+def test_a_request_that_outgrows_its_budget(dtype, hq, hkv, dim):
+    """Two layers: a prompt in two chunks with its weights gathered, eviction to a shorter table, single tokens over what is left, another eviction.  Each
+    step against the definition on the state that the GPU has at that point."""
+    L, slots, W, F = 2, 40, 60, 3
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    gen = torch.Generator().manual_seed(4)
+    pool = torch.full((L, slots, 2, 16, hkv, dim), float("nan"), dtype=dt, device=DEV)
+    scale = float(np.float32(1) / np.sqrt(np.float32(dim)))
+    ctx = cb.calvo_create(L, hq, hkv, dim, cb.CALVO_BF16 if dtype == "bf16" else cb.CALVO_F32, slots, pool)
+    alloc = cb.calvo_pool_create(slots)
+    stride = 400
+    mass = [torch.zeros((L, 1, hkv, stride), device=DEV) for _ in range(2)]
+    table, cached = np.zeros(0, np.int32), 0
+    step = wh.OUT[dtype] if (dtype, dim) == ("bf16", 128) else 0.0
+
+    def forward(n):
+        """n new tokens through both layers; checks outputs and weights."""
+        nonlocal table, cached
+        more = -(-(cached + n) // 16) - len(table)
+        if more:
+            table = np.concatenate([table, cb.calvo_pool_reserve(alloc, more)])
+        q = torch.randn((L, n, hq, dim), generator=gen).to(dt)
+        k, v = (torch.randn((L, n, hkv, dim), generator=gen).to(dt) for _ in range(2))
+        dq, dk, dv = q.to(DEV), k.to(DEV), v.to(DEV)
+        out, lse = torch.empty_like(dq), torch.empty((L, n, hq), device=DEV)
+        before = mass[0].cpu()
+        torch.cuda.synchronize()
+        plan = cb.calvo_window_prepare(ctx, [cb.make_window_request(table, cached, n)], W, F)
+        for l in range(L):
+            cb.calvo_window_attn(plan, l, dq[l], dk[l], dv[l], out[l], lse[l])
+            cb.calvo_attn_mass(plan, l, dq[l], lse[l], mass[0][l], mass[0][l], 1, stride)
+        cb.calvo_window_destroy(plan)
+        torch.cuda.synchronize()
+        for l in range(L):
+            p64 = pool[l].cpu().double().numpy()
+            for t in range(n):
+                assert torch.equal(pool[l, table[(cached + t) // 16], 0, (cached + t) % 16].cpu(), k[l, t])
+            q64 = q[l].double().numpy()
+            w_out, w_lse, mag, reach = wo.attn(p64, q64, table, cached, n, W, F, scale)
+            ds = wh.score_error(reach, dim)
+            keys = min(cached + n, W + F)
+            tol = mag * (2 * ds[..., None] + (2 * keys + 64) * U32 + step) + wh.OUT[dtype] * (np.abs(w_out) + mag * 2 ** -7)
+            assert (np.abs(out[l].cpu().double().numpy() - w_out) <= tol).all()
+            g_lse = lse[l].cpu().double().numpy()
+            assert (np.abs(g_lse - w_lse) <= ds + (2 * keys + 64) * U32 + 8 * U32 * (np.abs(w_lse) + reach)).all()
+            want = wo.mass(p64, q64, g_lse, table, cached, n, W, F, scale, before[l, 0].double().numpy())
+            got = mass[0][l, 0, :, :cached + n].cpu().double().numpy()
+            tol = np.abs(want) * (ds.max() + 8 * U32 * np.abs(g_lse).max() + (2 * n * hq // hkv + 64) * U32) + 1e-35
+            assert (np.abs(got - want) <= tol).all()
+        cached += n
+
+    def evict(keep, first, last):
+        nonlocal table, cached
+        new = cb.calvo_pool_reserve(alloc, -(-keep // 16))
+        kept = torch.zeros((L, 1, hkv, keep), dtype=torch.int32, device=DEV)
+        old, weights = pool.clone(), mass[0].cpu().numpy()
+        mass[1].zero_()
+        torch.cuda.synchronize()
+        cb.calvo_kv_evict(ctx, [cb.make_evict_request(table, cached, new, keep, first, last)], 0, L, mass[0], 1, stride, kept, keep, mass[1], stride)
+        torch.cuda.synchronize()
+        j = np.arange(keep)
+        for l in range(L):
+            for g in range(hkv):
+                at = wo.choose(weights[l, 0, g], cached, keep, first, last)
+                assert np.array_equal(kept[l, 0, g].cpu().numpy(), at)
+                assert np.array_equal(mass[1][l, 0, g, :keep].cpu().numpy(), weights[l, 0, g][at])
+                for half in (0, 1):
+                    assert torch.equal(pool[l, new[j // 16], half, j % 16, g], old[l, table[at // 16], half, at % 16, g])
+        cb.calvo_pool_release(alloc, table)
+        table, cached = new, keep
+        mass.reverse()
+
+    try:
+        forward(101)
+        forward(37)
+        evict(50, 4, 16)
+        for _ in range(5):
+            forward(1)
+        evict(33, 0, 8)
+        forward(20)
+        forward(1)
+        assert cb.calvo_pool_counts(alloc)["used"] == -(-cached // 16)
+    finally:
+        cb.calvo_pool_destroy(alloc)
+        cb.calvo_destroy(ctx)
+
+
+def test_everything_visible_is_the_causal_attention():
+    """Against calvo_prefill_attn on the same batch: whole cached blocks, no window."""
+    c = Case([(64, 40), (0, 17), (512, 3)], 8, 2, 128, seed=21)
+    got = c.run(FULL)
+    pool, q, k, v = (x.to(DEV) for x in (c.pool, c.q, c.k, c.v))
+    out = torch.empty_like(q)
+    torch.cuda.synchronize()
+    ctx = c.create(pool)
+    cb.calvo_prefill_attn(ctx, 0, q[0], k[0], v[0], out[0], [cb.make_request(None, 0, t, a // 16, n, a // 16) for t, (a, n) in zip(c.tables, c.lens)],
+                          c.cu.astype(np.int32))
+    cb.calvo_destroy(ctx)
+    # each is within two half steps of bf16 (weights and output) of the exact value, relative to the weighted |V|, which is below 4.5 here
+    assert (got["out"].float() - out.cpu().float()).abs().max() <= 2 * 2 * 2.0 ** -8 * float(c.v.float().abs().max())
+
+
+def test_plans_in_turn():
+    """Two batches alive at once, their calls interleaved over layers; a third one takes the first one's buffer while its launches are queued."""
+    a, b = Case([(300, 70), (900, 3)], 8, 2, 64, seed=1, layers=2), Case([(40, 1), (200, 20)], 8, 2, 64, seed=2, layers=2)
+    want = [x.run(100, 4) for x in (a, b)]
+    slots = a.slots + b.slots
+    pool = torch.cat([a.pool, b.pool], dim=1).to(DEV)
+    dev = [[x.to(DEV) for x in (c.q, c.k, c.v)] for c in (a, b)]
+    out = [torch.empty_like(d[0]) for d in dev]
+    again = torch.empty_like(dev[0][0])
+    torch.cuda.synchronize()
+    ctx = cb.calvo_create(2, 8, 2, 64, cb.CALVO_BF16, slots, pool)
+    try:
+        reqs = [a.requests(), [cb.make_window_request(t + a.slots, c, n, i) for i, (t, (c, n)) in enumerate(zip(b.tables, b.lens))]]
+        plans = [cb.calvo_window_prepare(ctx, r, 100, 4) for r in reqs]
+        for l in range(2):
+            for p, d, o in zip(plans, dev, out):
+                cb.calvo_window_attn(p, l, d[0][l], d[1][l], d[2][l], o[l])
+        for p in plans:
+            cb.calvo_window_destroy(p)
+        for _ in range(12):
+            p = cb.calvo_window_prepare(ctx, reqs[0], 100, 4)
+            cb.calvo_window_attn(p, 1, dev[0][0][1], None, None, again[1])
+            cb.calvo_window_destroy(p)
+    finally:
+        cb.calvo_destroy(ctx)
+    for o, w in zip(out, want):
+        assert torch.equal(o.cpu(), w["out"])
+    assert torch.equal(again[1].cpu(), want[0]["out"][1])
+
+
+@pytest.mark.parametrize("dtype,dim,lens", [("bf16", 128, [(500, 1), (2000, 1)]), ("bf16", 128, [(300, 90), (64, 33)]), ("f32", 64, [(301, 20), (10, 1)])])
+def test_captured_graph(dtype, dim, lens):
+    """Append, attention and weights of two layers in a graph, replayed over other inputs with eager calls of another plan in between."""
+    c = Case(lens, 8, 2, dim, dtype, seed=31, layers=2)
+    stream = torch.cuda.Stream()
+    pool, q, k, v = (x.to(DEV) for x in (c.pool, c.q, c.k, c.v))
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:-1], device=DEV)
+    rows, stride = len(lens), c.stride()
+    mass = torch.zeros((2, rows, 2, stride), device=DEV)
+    torch.cuda.synchronize()
+    ctx = c.create(pool, stream.cuda_stream)
+
+    def calls(plan):
+        for l in range(2):
+            cb.calvo_window_attn(plan, l, q[l], k[l], v[l], out[l], lse[l])
+            cb.calvo_attn_mass(plan, l, q[l], lse[l], None, mass[l], rows, stride)
+
+    try:
+        plan, other = (cb.calvo_window_prepare(ctx, c.requests(), 150, 4) for _ in range(2))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            with pytest.raises(cb.CalvoError, match="captured"):
+                cb.calvo_window_prepare(ctx, c.requests(), 150, 4)
+            with pytest.raises(cb.CalvoError, match="captured"):
+                cb.calvo_kv_evict(ctx, [], 0, 2, mass, rows, stride, mass, 1)
+            calls(plan)
+        for rep in range(4):
+            gen = torch.Generator().manual_seed(rep)
+            for x in (q, k, v):
+                x.copy_(torch.randn(x.shape, generator=gen).to(x.dtype))
+            torch.cuda.synchronize()
+            calls(other)
+            torch.cuda.synchronize()
+            want = [x.clone() for x in (out, lse, mass, pool)]
+            for x in (out, lse, mass):
+                x.zero_()
+            pool.copy_(c.pool)
+            torch.cuda.synchronize()
+            with torch.cuda.stream(stream):
+                graph.replay()
+            torch.cuda.synchronize()
+            as_int = torch.int16 if dtype == "bf16" else torch.int32
+            assert torch.equal(out, want[0]) and torch.equal(lse, want[1]) and torch.equal(mass, want[2])
+            assert torch.equal(pool.view(as_int), want[3].view(as_int))
+        del graph
+        cb.calvo_window_destroy(plan)
+        cb.calvo_window_destroy(other)
+    finally:
+        cb.calvo_destroy(ctx)
+
+
+def test_attention_waits_for_the_load(monkeypatch):
+    """The blocks are loaded by the context's own stage, slowed down on the host and on the device; the calls are queued at once."""
+    monkeypatch.setenv("CALVO_TEST_SCATTER_DELAY_US", "3000")
+    c = Case([(320, 1)], 8, 2, 128, seed=41, layers=2)
+    host = torch.empty((2, 20, 2, 16, 2, 128), dtype=c.dt, pin_memory=True)
+    host.copy_(c.pool[:, c.tables[0][:20].tolist()])
+    pool = torch.full(c.pool.shape, float("nan"), dtype=c.dt, device=DEV)
+    q, k, v = (x.to(DEV) for x in (c.q, c.k, c.v))
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:-1], device=DEV)
+    mass, kept = torch.zeros((2, 1, 2, 321), device=DEV), torch.zeros((2, 1, 2, 16), dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    ctx = cb.calvo_create(2, 8, 2, 128, cb.CALVO_BF16, c.slots, pool, staging_bytes=1 << 20)
+    try:
+        cb.calvo_kv_ingest(ctx, [cb.make_request(host, host[0].numel() * 2, c.tables[0], 20, 0)], 0, 2)
+        plan = cb.calvo_window_prepare(ctx, c.requests(), 200, 4)
+        for l in range(2):
+            cb.calvo_window_attn(plan, l, q[l], k[l], v[l], out[l], lse[l])
+            cb.calvo_attn_mass(plan, l, q[l], lse[l], None, mass[l], 1, 321)
+        cb.calvo_kv_evict(ctx, [cb.make_evict_request(c.tables[0], 321, c.free[:1], 16)], 0, 2, mass, 1, 321, kept, 16)
+        cb.calvo_window_destroy(plan)
+    finally:
+        cb.calvo_destroy(ctx)
+    got = {"out": out.cpu(), "lse": lse.cpu(), "mass": mass.cpu()}
+    for l in range(2):
+        wh.check_attn(c, got, 200, 4, l, wh.OUT["bf16"])
+        for g in range(2):
+            at = wo.choose(mass[l, 0, g].cpu().numpy(), 321, 16, 0, 0)
+            assert np.array_equal(kept[l, 0, g].cpu().numpy(), at)
+            j = np.arange(16)
+            assert torch.equal(pool[l, int(c.free[0]), 0, j, g], pool[l, c.tables[0][at // 16], 0, at % 16, g])
+
+
+def test_offsets_past_32_bits():
+    """A pool layer of more than 4 GiB, its last slots in use; weights and places in rows far apart."""
+    hkv, dim = 8, 256
+    slots = (5 << 30) // (2 * 16 * hkv * dim * 2)
+    pool = torch.zeros((1, slots, 2, 16, hkv, dim), dtype=torch.bfloat16, device=DEV)
+    c = Case([(100, 1), (70, 40)], 16, hkv, dim, seed=51)
+    high = slots - 1 - np.arange(c.slots)
+    pool[:, high.tolist()] = c.pool.to(DEV)
+    q, k, v = (x.to(DEV) for x in (c.q, c.k, c.v))
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:-1], device=DEV)
+    stride = 300 << 20                                      # floats: rows of KV heads 1.2 GB apart
+    mass = torch.zeros(2 * hkv * stride, device=DEV)
+    torch.cuda.synchronize()
+    ctx = cb.calvo_create(1, 16, hkv, dim, cb.CALVO_BF16, slots, pool)
+    try:
+        plan = cb.calvo_window_prepare(ctx, [cb.make_window_request(high[t], a, n, i) for i, (t, (a, n)) in enumerate(zip(c.tables, c.lens))], 50, 4)
+        cb.calvo_window_attn(plan, 0, q[0], k[0], v[0], out[0], lse[0])
+        cb.calvo_attn_mass(plan, 0, q[0], lse[0], None, mass, 2, stride)
+        cb.calvo_window_destroy(plan)
+        dst = np.array([5, 6], np.int32)
+        kept = torch.zeros((1, 1, hkv, 20), dtype=torch.int32, device=DEV)
+        cb.calvo_kv_evict(ctx, [cb.make_evict_request(high[c.tables[1]], 110, dst, 20, 2, 4, 1)], 0, 1, mass, 2, stride, kept, 20)
+    finally:
+        cb.calvo_destroy(ctx)
+    near = mass.view(2, hkv, stride)[:, :, :c.stride()].cpu()
+    got = {"out": out.cpu(), "lse": lse.cpu(), "mass": torch.full((1, 3, hkv, c.stride()), -5.0)}
+    for r, (a, n) in enumerate(c.lens):
+        got["mass"][0, r, :, :a + n] = near[r, :, :a + n]
+    wh.check_attn(c, got, 50, 4)
+    wh.check_mass(c, got, 50, 4)
+    j = np.arange(20)
+    for g in range(hkv):
+        at = wo.choose(near[1, g].numpy(), 110, 20, 2, 4)
+        assert np.array_equal(kept[0, 0, g].cpu().numpy(), at)
+        assert torch.equal(pool[0, dst[j // 16], 1, j % 16, g], pool[0, high[c.tables[1]][at // 16].tolist(), 1, at % 16, g])
+
+
+def test_refusals():
+    c = Case([(20, 3)], 8, 2, 64, seed=61, layers=2)
+    pool, q, k, v = (x.to(DEV) for x in (c.pool, c.q, c.k, c.v))
+    out, lse, mass = torch.full_like(q, 7.0), torch.full(q.shape[:-1], 7.0, device=DEV), torch.full((2, 2, 2, 30), 7.0, device=DEV)
+    kept = torch.full((2, 1, 2, 8), 7, dtype=torch.int32, device=DEV)
+    before = pool.clone()
+    torch.cuda.synchronize()
+    ctx = c.create(pool)
+
+    def refused(text, f):
+        with pytest.raises(cb.CalvoError) as e:
+            f()
+        assert e.value.code == cb.CALVO_EINVAL and text in str(e.value), e.value
+
+    try:
+        plan = cb.calvo_window_prepare(ctx, c.requests(), 10, 1)
+        attn = lambda layer=0, q_=q[0], k_=k[0], v_=v[0], o=out[0], s=lse[0]: cb.calvo_window_attn(plan, layer, q_, k_, v_, o, s)  # noqa: E731
+        refused("layer", lambda: attn(2))
+        refused("layer", lambda: attn(-1))
+        refused("NULL", lambda: attn(q_=None))
+        refused("NULL", lambda: attn(o=None))
+        refused("both", lambda: attn(v_=None))
+        refused("aligned", lambda: attn(q_=q.data_ptr() + 2))
+        refused("lse must be", lambda: attn(s=lse.data_ptr() + 2))
+        refused("overlaps", lambda: attn(o=q[0]))
+        refused("overlaps", lambda: attn(o=k[0]))
+        refused("overlaps", lambda: attn(s=out[0]))
+        refused("overlaps", lambda: attn(o=pool[0]))
+        refused("overlaps", lambda: attn(k_=pool[0]))
+        weigh = lambda layer=0, q_=q[0], s=lse[0], a=None, b=mass[0], rows=2, stride=30, last=0: cb.calvo_attn_mass(plan, layer, q_, s, a, b, rows, stride, last)  # noqa: E731
+        refused("layer", lambda: weigh(2))
+        refused("NULL", lambda: weigh(q_=None))
+        refused("NULL", lambda: weigh(s=None))
+        refused("NULL", lambda: weigh(b=None))
+        refused("negative", lambda: weigh(last=-1))
+        refused("mass_stride", lambda: weigh(stride=22))
+        refused("mass_row", lambda: weigh(rows=0))
+        refused("overlaps", lambda: weigh(a=mass.data_ptr() + 4))
+        refused("overlaps", lambda: weigh(b=lse))
+        refused("overlaps", lambda: weigh(b=pool))
+        same = cb.calvo_window_prepare(ctx, [cb.make_window_request(c.tables[0], 20, 0, 1), cb.make_window_request(c.tables[0], 10, 0, 1)], 10)
+        refused("differ", lambda: cb.calvo_attn_mass(same, 0, None, None, None, mass, 2, 30))
+        cb.calvo_window_destroy(same)
+        evict = lambda b=0, e=2, m=mass, rows=2, stride=30, k_=kept, ks=8, o=None, os=0, n=20, keep=8: cb.calvo_kv_evict(  # noqa: E731
+            ctx, [cb.make_evict_request(c.tables[0], n, c.free[:1], keep)], b, e, m, rows, stride, k_, ks, o, os)
+        refused("layers", lambda: evict(e=3))
+        refused("layers", lambda: evict(b=2, e=1))
+        refused("NULL", lambda: evict(m=None))
+        refused("NULL", lambda: evict(k_=None))
+        refused("mass_stride", lambda: evict(stride=19))
+        refused("kept_stride", lambda: evict(ks=7))
+        refused("out_stride", lambda: evict(o=lse, os=7))
+        refused("aligned", lambda: evict(m=mass.data_ptr() + 1))
+        refused("overlaps", lambda: evict(o=mass, os=8))
+        refused("overlaps", lambda: evict(k_=pool))
+        cb.calvo_window_destroy(plan)
+    finally:
+        cb.calvo_destroy(ctx)
+    torch.cuda.synchronize()
+    assert bool((out == 7).all()) and bool((lse == 7).all()) and bool((mass == 7).all()) and bool((kept == 7).all())
+    assert torch.equal(pool.view(torch.int16), before.view(torch.int16))
+
+
+def test_empty_batches():
+    c = Case([(20, 0)], 8, 2, 64, seed=71)
+    pool = c.pool.to(DEV)
+    torch.cuda.synchronize()
+    ctx = c.create(pool)
+    try:
+        for reqs in ([], c.requests()):
+            plan = cb.calvo_window_prepare(ctx, reqs, 10, 1)
+            cb.calvo_window_attn(plan, 0, None, None, None, None)
+            cb.calvo_window_destroy(plan)
+        plan = cb.calvo_window_prepare(ctx, [], 10, 1)
+        cb.calvo_attn_mass(plan, 0, None, None, None, None, 0, 0)
+        cb.calvo_window_destroy(plan)
+        cb.calvo_kv_evict(ctx, [], 0, 1, None, 0, 0, None, 0)
+        cb.calvo_kv_evict(ctx, [cb.make_evict_request([], 0, [], 0)], 0, 1, None, 0, 0, None, 0)
+    finally:
+        cb.calvo_destroy(ctx)
