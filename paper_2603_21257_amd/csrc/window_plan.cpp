@@ -72,6 +72,11 @@ void make_tiles(Candidate& c, const std::vector<WindowLens>& lens, int group, in
   std::stable_sort(c.tiles.begin(), c.tiles.end(), [](const PlanTile& a, const PlanTile& b) { return a.n_sub > b.n_sub; });
 }
 
+// in the units of attn_rows_shape
+RowsShape few_rows_shape(bool f32, int head_dim) {
+  return {kFewRows, f32 ? (head_dim <= 64 ? 14 : 28) : (head_dim <= 64 ? 5 : 8), 60, 1};
+}
+
 }  // namespace
 
 void plan_window(const WindowShape& s, const std::vector<WindowLens>& lens, int32_t window, int32_t n_first, WindowPlan& out) {
@@ -82,21 +87,29 @@ void plan_window(const WindowShape& s, const std::vector<WindowLens>& lens, int3
   for (const WindowLens& l : lens) total += l.n_new;
   if (total == 0) return;
 
-  // Single tokens: half the rows of the smaller tiling, where that has 32, leave the combination of the waves half as long (us a call of one caller, 32
-  // / 16 rows, 32Q/8KV: 4096+1 behind 4096 15.4 / 14.0, 20000+1 behind 16384 23.3 / 20.7), and none of the other tilings is looked at
+  // Up to 128-wide heads there is a tiling of 16 rows as well.  Single tokens take it: it leaves the combination of the waves half as long (us a call of
+  // one caller, 32 / 16 rows, 32Q/8KV: 4096+1 behind 4096 15.4 / 14.0, 20000+1 behind 16384 23.3 / 20.7), and none of the others is looked at
   // (planning 32 requests takes 40 us, 5 this way).
-  bool few = s.force_tile == 0 && s.force_variant == 0 && s.head_dim <= 128;
-  for (const WindowLens& l : lens) few &= (int64_t)l.n_new * group <= kFewRows;
+  const bool has_few = s.force_tile == 0 && s.head_dim <= 128;
+  bool few = has_few && s.force_variant == 0, one_tile = true;
+  for (const WindowLens& l : lens) {
+    few &= (int64_t)l.n_new * group <= kFewRows;
+    one_tile &= (int64_t)l.n_new * group <= attn_rows_shape(s.f32, s.head_dim, false).tile_rows;
+  }
+  // Batches that leave most of the chip idle take it where the replay is shorter (one caller, 32 / 16 rows: fp32 D = 64 8Q/2KV 1000+128 behind 300 15.8 /
+  // 12.7, bf16 1000+64 14.4 / 13.1, 32Q/8KV 4000+100 behind 1024 14.9 / 14.1; not 16Q/4KV 4111+300 behind 2048 21.2 / 30.4, fp32 8Q/2KV 4000+200
+  // 30.0 / 33.8), and where that does not cost the launch that stores the new rows (one_tile).
   Candidate best;
-  for (const bool large : {false, true}) {
-    if (large && (few || !attn_rows_has_large(s.f32, s.head_dim) || s.force_tile == 1)) break;
+  for (const int kind : {0, 1, 2}) {
+    if (kind == 1 && (!has_few || (one_tile && !few))) continue;
+    if (kind == 2 && (few || !attn_rows_has_large(s.f32, s.head_dim) || s.force_tile == 1)) break;
+    if (kind == 0 && few) continue;
     Candidate c;
-    c.shape = attn_rows_shape(s.f32, s.head_dim, large);
-    if (few && !large) c.shape.tile_rows = kFewRows;
+    c.shape = kind == 1 ? few_rows_shape(s.f32, s.head_dim) : attn_rows_shape(s.f32, s.head_dim, kind == 2);
     c.params = rows_plan_params(c.shape, s.n_kv_heads, s.n_cus, s.force_splits);
     make_tiles(c, lens, group, window, n_first);
     c.want = plan_pieces(c.tiles, c.params, kMostSlots / c.shape.slots, &c.cost);
-    if (!large || s.force_tile == 2 || 2. * c.cost.span + c.cost.load < 0.97 * (2. * best.cost.span + best.cost.load)) best = std::move(c);
+    if (best.tiles.empty() || (kind == 2 && s.force_tile == 2) || 2. * c.cost.span + c.cost.load < 0.97 * (2. * best.cost.span + best.cost.load)) best = std::move(c);
   }
   if (!s.f32 && s.head_dim == 128 && s.force_variant != 5 && !few) {
     Candidate pipe, duo;
