@@ -748,15 +748,21 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
         qk(ring_slot(j), Tag<2 * H>{}, s2);
         if constexpr (WIN) {
           const int window = pe->window, n_first = pe->n_first;
+          if (k0 + 31 > pq_min || (k0 <= pq_min + 31 - window && k0 + 31 >= n_first)) {
 #pragma unroll
-          for (int kb = 0; kb < 2; kb++)
+            for (int q = 0; q < 2; q++) {
+              // a row sees the keys from lo on, `many` of them, and the first ones
+              const unsigned pos = (unsigned)(pq_min + 16 * q + c), lo = (unsigned)max(0, (int)pos - window + 1), many = pos + 1 - lo;
+              const unsigned first = min((unsigned)n_first, pos + 1);
 #pragma unroll
-            for (int q = 0; q < 2; q++)
+              for (int kb = 0; kb < 2; kb++)
 #pragma unroll
-              for (int r = 0; r < 4; r++) {
-                const int key = k0 + 16 * kb + 4 * g + r, pos = pq_min + 16 * q + c;
-                if (key > pos || (key <= pos - window && key >= n_first)) s2[kb][q][r] = -INFINITY;
-              }
+                for (int r = 0; r < 4; r++) {
+                  const unsigned key = (unsigned)(k0 + 16 * kb + 4 * g + r);
+                  if (!((key - lo < many) | (key < first))) s2[kb][q][r] = -INFINITY;
+                }
+            }
+          }
         } else if (k0 + 31 > pq_min) {
 #pragma unroll
           for (int kb = 0; kb < 2; kb++)

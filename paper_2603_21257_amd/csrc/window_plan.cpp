@@ -125,13 +125,21 @@ void plan_window(const WindowShape& s, const std::vector<WindowLens>& lens, int3
     //   window 1024   4096+1 17.3 / 28.3 / 35.9      4096+64 21.4 / 30.8 / 46.1    4096+256 23.4 / 30.7 / 46.4    4096+1024 59.1 / 36.3 / 50.9
     //   window 16384  20000+1 24.9 / 26.6 / 30.7     20000+64 51.1 / 37.5 / 47.8   20000+256 142 / 79.1 / 81.1    20000+1024 504 / 250 / 242
     //   window 256    0+500 20.5 / 20.6 / 31.5       0+2000 71.9 / 32.0 / 39.2     0+8192 253 / 93.5 / 135
-    // Among the pipelined ones the larger tiles read K and V half as often, the smaller ones have two workgroups on a CU whose sub-tiles outside the steady
-    // loop hide each other's: kAttnDuo / kAttnPipe, 0+32768 behind 1024 712 / 774, 2048 1089 / 1169, 4096 1800 / 1862, 8192 3260 / 3228; 16384+2048
-    // behind 2048 80.0 / 82.5, 8192 245 / 232; 60000+4096 behind everything 3317 / 3157; 30000+256 128 / 124; 4096+4096 (40Q/8KV) behind 4096 337 / 424.
-    constexpr int kLongList = 200, kLongLaunch = 250;
+    // Among the pipelined ones the larger tiles read K and V half as often, the smaller ones have two workgroups on a CU whose starts, ends and sub-tiles
+    // outside the steady loop hide each other.  Those sub-tiles grow with the tokens of a tile (64, 128 or 256 at four, two or one query heads to a workgroup):
+    // the sides cross where a list has some two sub-tiles for every token.  kAttnPipe / kAttnDuo, us a call of one caller, 16384+2048 tokens and 0+16384
+    // behind 2048, 4096, 8192, 16384:
+    //   32Q/8KV  76.3 / 76.2  122 / 128   214 / 232   403 / 449      569 / 541   861 / 847    1300 / 1330  1634 / 1710
+    //   16Q/8KV  63.2 / 53.1  86.4 / 83.0 133 / 140   227 / 254      305 / 271   470 / 443    664 / 698    836 / 881
+    //   40Q/8KV  (320 workgroups on 256 CUs: 740 / 622 at 16384)     779 / 717   1138 / 1077  1679 / 1655  2073 / 2130
+    // Short launches are the smaller tiles' (20000+700 behind 4096 71.8 / 71.3, 20000+64 behind 16384 47.8 / 37.5), and so are those that fill the last round
+    // of CUs badly, where a workgroup of the smaller tiles has its CU to itself.
+    constexpr double kSubsPerToken = 1.9, kLongLaunch = 140., kFilled = 0.9;
     int64_t subs = 0;
     for (const PlanTile& t : pipe.tiles) subs += t.n_sub;
-    const bool larger = s.force_variant ? s.force_variant == kAttnPipe : subs >= kLongList * (int64_t)pipe.tiles.size() && pipe.cost.span >= kLongLaunch;
+    const bool larger = s.force_variant ? s.force_variant == kAttnPipe
+                                        : (double)subs >= kSubsPerToken * pipe.tile_tokens * (double)pipe.tiles.size() && pipe.cost.span >= kLongLaunch &&
+                                              pipe.cost.load >= kFilled * pipe.cost.span && pipe.cost.span <= 1.03 * duo.cost.span;
     if (s.force_variant || 3. + 0.12 * best.cost.span >= 0.6 * duo.cost.span) best = std::move(larger ? pipe : duo);
   }
   out.variant = best.variant;
