@@ -210,8 +210,11 @@ struct EvictParams {
   int32_t row_chunks;        // 16-byte chunks of one head's K (or V) of a token
   int32_t max_tokens, max_keep;   // most tokens that a request has and keeps
 };
-hipError_t launch_evict_select(const EvictParams& p, hipStream_t stream);
-hipError_t launch_evict_move(const EvictParams& p, hipStream_t stream);
+// The words behind reqs (descriptors, then tables) of a small call go along as an argument of its launches: words is their HOST address then and
+// reqs and tables are not looked at; else NULL
+constexpr int kEvictArgWords = 768;
+hipError_t launch_evict_select(const EvictParams& p, const int32_t* words, int n_words, hipStream_t stream);
+hipError_t launch_evict_move(const EvictParams& p, const int32_t* words, int n_words, hipStream_t stream);
 
 // The pipelined bf16 / head-dim-128 kernels (attn_pipeline.h).  The *_prepare calls raise the
 // kernels' dynamic LDS limit; once per device, before the first launch.

@@ -492,24 +492,28 @@ int kv_evict(calvo_ctx* c, const calvo_evict_request* reqs, int n_reqs, int laye
 
   constexpr size_t kReq = sizeof(EvictDesc) / 4;
   const size_t words = ((size_t)n_reqs * kReq + (size_t)table_words + 3) / 4 * 4;
+  const bool in_args = words <= (size_t)kEvictArgWords;
+  int32_t args[kEvictArgWords];
   StepBuf buf;
-  if ((rc = take_buf(c, words * 4, words * 4, buf)) != CALVO_OK) { free_buf(buf); return rc; }
+  if (!in_args && (rc = take_buf(c, words * 4, words * 4, buf)) != CALVO_OK) { free_buf(buf); return rc; }
+  int32_t* const h = in_args ? args : buf.h;
   int32_t at = 0;
-  int32_t* tables = buf.h + (size_t)n_reqs * kReq;
+  int32_t* tables = h + (size_t)n_reqs * kReq;
   for (int r = 0; r < n_reqs; r++) {
     const calvo_evict_request& q = reqs[r];
     const int32_t ns = q.n_keep ? (int32_t)blocks_of(q.n_tokens) : 0, nd = (int32_t)blocks_of(q.n_keep);
     const EvictDesc d = {at, at + ns, q.n_keep ? q.n_tokens : 0, q.n_keep, q.n_first, q.n_last, q.n_keep ? q.mass_row : 0, 0};
-    memcpy(buf.h + (size_t)r * kReq, &d, sizeof d);
+    memcpy(h + (size_t)r * kReq, &d, sizeof d);
     if (ns) memcpy(tables + at, q.src_table, (size_t)ns * 4);
     if (nd) memcpy(tables + at + ns, q.dst_table, (size_t)nd * 4);
     at += ns + nd;
   }
-  rc = upload(c, buf, words);
+  const int n_words = (int)((size_t)n_reqs * kReq) + at;
+  if (!in_args) rc = upload(c, buf, words);
   if (rc == CALVO_OK) {
     EvictParams p{};
     p.pool = (unsigned char*)cf.pool + (int64_t)layer_begin * c->layer_bytes;
-    p.reqs = (const EvictDesc*)buf.d; p.tables = buf.d + (size_t)n_reqs * kReq;
+    p.reqs = (const EvictDesc*)buf.d; p.tables = in_args ? nullptr : buf.d + (size_t)n_reqs * kReq;
     p.mass = mass; p.mass_out = mass_out; p.kept = kept;
     p.layer_bytes = c->layer_bytes;
     p.mass_stride = mass_stride; p.mass_layer = (int64_t)mass_rows * cf.n_kv_heads * mass_stride;
@@ -519,11 +523,11 @@ int kv_evict(calvo_ctx* c, const calvo_evict_request* reqs, int n_reqs, int laye
     p.row_chunks = (int32_t)((size_t)cf.head_dim * c->elt / 16);
     p.max_tokens = (int32_t)longest;
     p.max_keep = max_keep;
-    hipError_t e = launch_evict_select(p, c->s_compute);
-    if (e == hipSuccess) e = launch_evict_move(p, c->s_compute);
+    hipError_t e = launch_evict_select(p, in_args ? args : nullptr, n_words, c->s_compute);
+    if (e == hipSuccess) e = launch_evict_move(p, in_args ? args : nullptr, n_words, c->s_compute);
     if (e != hipSuccess) rc = fail_hip(e, "launch of calvo_kv_evict");
   }
-  give_buf(c, buf);
+  if (!in_args) give_buf(c, buf);
   return rc;
 }
 

@@ -10,6 +10,9 @@
 // Then one exchange of counts tells every wave where its kept tokens go.  256 rows of 16384 tokens: 20 us (bins of the leading eight bits 27;
 // the rank found bit by bit, tokens counted in the waves' masks, 37).
 // Move: one workgroup per destination block, bytes in, bytes out, at the rate of a large copy.
+#include <cstring>
+#include <type_traits>
+
 #include "attn_common.h"
 
 namespace calvo {
@@ -25,12 +28,33 @@ __device__ inline uint32_t rank_of(float x) {
   return x != x ? kNaN : k;
 }
 
+// Descriptors and tables: in device memory, or for small calls in the launch's arguments, which saves the upload in front of it and its event (one
+// request of 2011 tokens, 4 layers, fp32: 18.3 -> 12.7 us a call)
+struct NoWords {};
+struct ArgWords {
+  int32_t w[kEvictArgWords];
+};
+constexpr int kDescWords = sizeof(EvictDesc) / 4;
+template <typename W>
+__device__ inline EvictDesc desc_of(const EvictParams& p, const W& words, int r) {
+  if constexpr (std::is_same<W, NoWords>::value) return p.reqs[r];
+  else {
+    const int32_t* w = words.w + kDescWords * r;
+    return {w[0], w[1], w[2], w[3], w[4], w[5], w[6], 0};
+  }
+}
+template <typename W>
+__device__ inline int32_t table_at(const EvictParams& p, const W& words, int i) {
+  if constexpr (std::is_same<W, NoWords>::value) return p.tables[i];
+  else return words.w[kDescWords * p.n_reqs + i];
+}
+
 constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 512;
 
 // V: steps of 64 positions of a wave whose weights are in registers at a time.  No branch stands between their loads (one for each step made
 // them wait for one another: 16384 tokens 61 us).
-template <int V>
-__global__ void __launch_bounds__(kThreads) evict_select_kernel(EvictParams p) {
+template <int V, typename W>
+__global__ void __launch_bounds__(kThreads) evict_select_kernel(EvictParams p, W words) {
   __shared__ int hist[kBins];
   __shared__ uint32_t ends[kWaves][2];                         // smallest and largest rank of a wave
   __shared__ int pick[3];                                      // bin, rank that is left inside it, weights in it
@@ -38,7 +62,7 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(EvictParams p) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = blockIdx.x % p.n_kv_heads, r = blockIdx.x / p.n_kv_heads % p.n_reqs, layer = blockIdx.x / p.n_kv_heads / p.n_reqs;
-  const EvictDesc d = p.reqs[r];
+  const EvictDesc d = desc_of(p, words, r);
   if (d.n_keep == 0) return;                                   // then its counts are 0: there is no position to read at
   const float* mass = p.mass + layer * p.mass_layer + ((int64_t)d.mass_row * p.n_kv_heads + g) * p.mass_stride;
   int32_t* kept = p.kept + (((int64_t)layer * p.n_reqs + r) * p.n_kv_heads + g) * p.kept_stride;
@@ -180,44 +204,62 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(EvictParams p) {
   }
 }
 
-__global__ void __launch_bounds__(256) evict_move_kernel(EvictParams p) {
-  const EvictDesc d = p.reqs[blockIdx.y];
+template <typename W>
+__global__ void __launch_bounds__(256) evict_move_kernel(EvictParams p, W words) {
+  const EvictDesc d = desc_of(p, words, blockIdx.y);
   const int block = blockIdx.x;
   const int rows = min(kBlockTokens, d.n_keep - block * kBlockTokens);   // of the destination block
   if (rows <= 0) return;
   const int64_t half = (int64_t)kBlockTokens * p.n_kv_heads * p.row_chunks;   // 16-byte chunks of a block's K (or V)
   u32x4* pool = (u32x4*)(p.pool + blockIdx.z * p.layer_bytes);
   const int32_t* kept = p.kept + ((int64_t)blockIdx.z * p.n_reqs + blockIdx.y) * p.n_kv_heads * p.kept_stride + block * kBlockTokens;
-  const int32_t* src = p.tables + d.src_off;
-  const int64_t dst = (int64_t)p.tables[d.dst_off + block] * 2 * half;
+  const int64_t dst = (int64_t)table_at(p, words, d.dst_off + block) * 2 * half;
   const int per_row = p.n_kv_heads * p.row_chunks, n = rows * per_row;
   for (int i = threadIdx.x; i < n; i += 256) {
     const int j = i / per_row, in_row = i - j * per_row, g = in_row / p.row_chunks;
     const int pos = kept[g * p.kept_stride + j];
-    const int64_t at = (int64_t)src[pos / kBlockTokens] * 2 * half + (int64_t)(pos % kBlockTokens) * per_row + in_row;
+    const int64_t at = (int64_t)table_at(p, words, d.src_off + pos / kBlockTokens) * 2 * half + (int64_t)(pos % kBlockTokens) * per_row + in_row;
     const u32x4 k = pool[at], v = pool[at + half];
     pool[dst + i] = k;
     pool[dst + i + half] = v;
   }
 }
 
-}  // namespace evict
-
-hipError_t launch_evict_select(const EvictParams& p, hipStream_t stream) {
-  const unsigned grid = (unsigned)p.n_layers * (unsigned)p.n_reqs * (unsigned)p.n_kv_heads;
-  if (grid == 0) return hipSuccess;
-  const int64_t steps = ((int64_t)p.max_tokens + evict::kThreads - 1) / evict::kThreads;
-  if (steps <= 4) hipLaunchKernelGGL(evict::evict_select_kernel<4>, dim3(grid), dim3(evict::kThreads), 0, stream, p);
-  else if (steps <= 16) hipLaunchKernelGGL(evict::evict_select_kernel<16>, dim3(grid), dim3(evict::kThreads), 0, stream, p);
-  else hipLaunchKernelGGL(evict::evict_select_kernel<32>, dim3(grid), dim3(evict::kThreads), 0, stream, p);
+template <typename F>
+hipError_t with_words(const int32_t* words, int n_words, F&& launch) {
+  if (words) {
+    ArgWords a;
+    std::memcpy(a.w, words, (size_t)n_words * 4);
+    launch(a);
+  } else {
+    launch(NoWords{});
+  }
   return hipGetLastError();
 }
 
-hipError_t launch_evict_move(const EvictParams& p, hipStream_t stream) {
+}  // namespace evict
+
+hipError_t launch_evict_select(const EvictParams& p, const int32_t* words, int n_words, hipStream_t stream) {
+  using namespace evict;
+  const unsigned grid = (unsigned)p.n_layers * (unsigned)p.n_reqs * (unsigned)p.n_kv_heads;
+  if (grid == 0) return hipSuccess;
+  const int64_t steps = ((int64_t)p.max_tokens + kThreads - 1) / kThreads;
+  return with_words(words, n_words, [&](const auto& w) {
+    typedef typename std::decay<decltype(w)>::type W;
+    if (steps <= 4) hipLaunchKernelGGL((evict_select_kernel<4, W>), dim3(grid), dim3(kThreads), 0, stream, p, w);
+    else if (steps <= 16) hipLaunchKernelGGL((evict_select_kernel<16, W>), dim3(grid), dim3(kThreads), 0, stream, p, w);
+    else hipLaunchKernelGGL((evict_select_kernel<32, W>), dim3(grid), dim3(kThreads), 0, stream, p, w);
+  });
+}
+
+hipError_t launch_evict_move(const EvictParams& p, const int32_t* words, int n_words, hipStream_t stream) {
+  using namespace evict;
   if (p.max_keep <= 0 || p.n_reqs <= 0 || p.n_layers <= 0) return hipSuccess;
   const unsigned blocks = (unsigned)(p.max_keep + kBlockTokens - 1) / kBlockTokens;
-  hipLaunchKernelGGL(evict::evict_move_kernel, dim3(blocks, (unsigned)p.n_reqs, (unsigned)p.n_layers), dim3(256), 0, stream, p);
-  return hipGetLastError();
+  return with_words(words, n_words, [&](const auto& w) {
+    typedef typename std::decay<decltype(w)>::type W;
+    hipLaunchKernelGGL(evict_move_kernel<W>, dim3(blocks, (unsigned)p.n_reqs, (unsigned)p.n_layers), dim3(256), 0, stream, p, w);
+  });
 }
 
 }  // namespace calvo
