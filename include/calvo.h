@@ -290,7 +290,7 @@ typedef struct {
                                  the call only.  A slot that takes new tokens is in no other request's table of the batch */
   int32_t n_cached;           /* >= 0 */
   int32_t n_new;              /* >= 0 */
-  int32_t mass_row;           /* row of the request in the arrays of calvo_attn_mass */
+  int32_t mass_row;           /* row of the request in the arrays of calvo_attn_mass (-1: the plan is not used for it, and plans less) */
   int32_t reserved;           /* 0 */
 } calvo_window_request;
 

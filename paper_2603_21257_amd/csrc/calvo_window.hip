@@ -272,7 +272,8 @@ int window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, i
   plan_window({cf.dtype == CALVO_F32, cf.head_dim, cf.n_q_heads, cf.n_kv_heads, c->n_cus, c->force_splits, c->force_rows_tile, forced_variant()}, lens,
               window, n_first, w->plan);
   const int tile_keys = attn_mass_tile_keys(cf.dtype, cf.head_dim);
-  plan_mass(cf.n_q_heads / cf.n_kv_heads, cf.n_kv_heads, c->n_cus, tile_keys, lens, window, n_first, w->mass);
+  if (w->mass_rows_differ)                // else calvo_attn_mass refuses the plan
+    plan_mass(cf.n_q_heads / cf.n_kv_heads, cf.n_kv_heads, c->n_cus, tile_keys, lens, window, n_first, w->mass);
   const size_t n_mass = w->mass.items.size();
   if ((int64_t)n_mass * cf.n_kv_heads > INT32_MAX) return fail(CALVO_EINVAL, "too many tokens in the batch");
   const bool rows = w->plan.variant == kWindowRows;
@@ -418,7 +419,7 @@ int attn_mass(calvo_window* w, int layer, const void* q, const float* lse, const
   if (rc != CALVO_OK) return rc;
   if (cf.n_q_heads / cf.n_kv_heads > 4096) return fail(CALVO_EINVAL, "more than 4096 query heads to a KV head");
   if (mass_rows < 0 || last_rows < 0) return fail(CALVO_EINVAL, "mass_rows and last_rows must not be negative");
-  if (!w->mass.items.empty()) {
+  if (w->longest > 0) {
     if (!mass_out) return fail(CALVO_EINVAL, "mass_out is NULL");
     if (w->total > 0 && (!q || !lse)) return fail(CALVO_EINVAL, "q or lse is NULL");
     if (((uintptr_t)q & 15) != 0) return fail(CALVO_EINVAL, "q must be 16-byte aligned");
