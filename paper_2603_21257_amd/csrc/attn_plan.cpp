@@ -10,6 +10,8 @@
 #include <algorithm>
 #include <cstdlib>
 #include <functional>
+#include <utility>
+#include <vector>
 
 #include "../../include/calvo.h"
 
@@ -104,6 +106,31 @@ int plan_piece_len(int n_sub, int n_max, int want, const PlanParams& p) {
 // (64Q/8KV, 224 uncut) 38.9 uncut, 49.1 in two.
 constexpr double kAlone = 0.7;
 
+// Workgroup slots that become free at the same time: (time, how many), a min-heap of them
+using FreeSlots = std::vector<std::pair<int64_t, int64_t>>;
+
+// `n` pieces of the same cost, one after the other to the slot that is free first; returns the last one's end.  Whole entries move at a time: planning
+// is part of every call that a host thread makes (28096+28, 28304+61 and 38304+209 tokens behind 8192: a slot at a time @@OLD@@ us, @@NEW@@ this way).
+static int64_t place(FreeSlots& heap, int64_t n, int64_t cost) {
+  const auto later = std::greater<std::pair<int64_t, int64_t>>();
+  int64_t end = 0;
+  while (n > 0) {
+    std::pair<int64_t, int64_t> top = heap[0];
+    const int64_t taken = std::min(n, top.second);
+    n -= taken;
+    end = top.first + cost;                              // the top never falls
+    if (taken < top.second) {
+      heap[0].second -= taken;                           // still the smallest
+    } else {
+      std::pop_heap(heap.begin(), heap.end(), later);
+      heap.pop_back();
+    }
+    heap.push_back({end, taken});
+    std::push_heap(heap.begin(), heap.end(), later);
+  }
+  return end;
+}
+
 int plan_pieces(const std::vector<PlanTile>& tiles, const PlanParams& p, int64_t max_slots, PlanCost* found, double limit) {
   if (found) *found = {};
   if (p.force_splits) return p.force_splits;
@@ -123,18 +150,23 @@ int plan_pieces(const std::vector<PlanTile>& tiles, const PlanParams& p, int64_t
   int want = 1;
   double best = limit / 0.98;
   if (found) found->span = HUGE_VAL;
-  std::vector<int64_t> heap;
+  std::vector<std::pair<int, int64_t>> runs;        // tiles of equal length: sub-tiles, workgroups of all of them uncut
+  for (const PlanTile& t : tiles) {
+    if (runs.empty() || runs.back().first != t.n_sub) runs.push_back({t.n_sub, 0});
+    runs.back().second += p.n_head_groups;
+  }
+  FreeSlots heap;
   for (int n : p.long_pieces ? coarse : all) {
     if (n > 1 && wgs * n > (p.step_cost ? 4 : 16) * (int64_t)p.wg_slots) break;
     bool cut = false;
     int64_t end = 0, slots = 0, work = 0, longest = 0;
-    for (const PlanTile& t : tiles) {
-      const int len = plan_piece_len(t.n_sub, n_max, n, p);
-      const int np = (t.n_sub + len - 1) / len;
+    for (const auto& [n_sub, wgs_of] : runs) {
+      const int len = plan_piece_len(n_sub, n_max, n, p);
+      const int np = (n_sub + len - 1) / len;
       cut |= np > 1;
-      slots += (int64_t)np * p.n_head_groups;
-      work += ((np - 1) * cost_of(len) + cost_of(t.n_sub - (np - 1) * len)) * p.n_head_groups;
-      longest = std::max(longest, cost_of(std::min(len, t.n_sub)));
+      slots += np * wgs_of;
+      work += ((np - 1) * cost_of(len) + cost_of(n_sub - (np - 1) * len)) * wgs_of;
+      longest = std::max(longest, cost_of(std::min(len, n_sub)));
     }
     if (n > 1 && slots > max_slots) break;
     // no order of the pieces beats the average load or the longest piece: most candidates need no replay
@@ -144,18 +176,17 @@ int plan_pieces(const std::vector<PlanTile>& tiles, const PlanParams& p, int64_t
       if (!cut && n > 1) break;
       continue;
     }
-    heap.assign((size_t)p.wg_slots, 0);            // min-heap of the times at which workgroup slots become free
-    auto cmp = std::greater<int64_t>();
-    for (const PlanTile& t : tiles) {
-      const int len = plan_piece_len(t.n_sub, n_max, n, p);
-      const int np = (t.n_sub + len - 1) / len;
-      for (int k = 0; k < np; k++) {
-        const int64_t cost = cost_of(std::min(t.n_sub, (k + 1) * len) - k * len);
-        for (int h = 0; h < p.n_head_groups; h++) {
-          std::pop_heap(heap.begin(), heap.end(), cmp);
-          heap.back() += cost;
-          end = std::max(end, heap.back());
-          std::push_heap(heap.begin(), heap.end(), cmp);
+    if (slots <= p.wg_slots) {
+      end = longest;
+    } else {
+      heap.assign(1, {0, p.wg_slots});
+      for (const auto& [n_sub, wgs_of] : runs) {
+        const int len = plan_piece_len(n_sub, n_max, n, p);
+        const int np = (n_sub + len - 1) / len;
+        const int64_t at_once = np > 1 ? p.n_head_groups : wgs_of;
+        for (int64_t i = 0; i < wgs_of; i += at_once) {
+          end = std::max(end, place(heap, (np - 1) * at_once, cost_of(len)));
+          end = std::max(end, place(heap, at_once, cost_of(n_sub - (np - 1) * len)));
         }
       }
     }

@@ -98,10 +98,11 @@ void plan_window(const WindowShape& s, const std::vector<WindowLens>& lens, int3
   }
   // Batches that leave most of the chip idle take it where the replay is shorter (one caller, 32 / 16 rows: fp32 D = 64 8Q/2KV 1000+128 behind 300 15.8 /
   // 12.7, bf16 1000+64 14.4 / 13.1, 32Q/8KV 4000+100 behind 1024 14.9 / 14.1; not 16Q/4KV 4111+300 behind 2048 21.2 / 30.4, fp32 8Q/2KV 4000+200
-  // 30.0 / 33.8), and where that does not cost the launch that stores the new rows (one_tile).
+  // 30.0 / 33.8), and where that does not cost the launch that stores the new rows (one_tile); from four workgroups per CU on they are not
+  // replayed (of 100000 drawn batches 109 would have taken it).
   Candidate best;
   for (const int kind : {0, 1, 2}) {
-    if (kind == 1 && (!has_few || (one_tile && !few))) continue;
+    if (kind == 1 && (!has_few || (one_tile && !few) || (int64_t)best.tiles.size() * s.n_kv_heads > 4 * (int64_t)s.n_cus)) continue;
     if (kind == 2 && (few || !attn_rows_has_large(s.f32, s.head_dim) || s.force_tile == 1)) break;
     if (kind == 0 && few) continue;
     Candidate c;
