@@ -8,6 +8,11 @@
 // The four waves of a workgroup own tiles side by side and share the rows, which come straight from memory into LDS (global_load_lds), 16 KiB
 // a stage, two stages ahead; 16-byte chunks are XOR-swizzled on the way so that operand reads have no bank conflicts.  Where there are
 // many rows a tile is worked on by several workgroups, each with its part of them (MassItem); mass_add_kernel adds their sums in order.
+//
+// What bounds it (32Q/8KV, D = 128, bf16).  Few rows: reading K.  One new token each of 8 requests of 4096 to 20000 tokens 39 us, 4.9 TB/s, what
+// a large copy reaches.  Many: a score costs the vector ALU a fused multiply-add, an exponential and an addition, and the clock falls to 1.98 GHz under the
+// power of both units.  0+8192 tokens 313 us and 4.6 of addition, 880 TFLOP/s (960 between the ends); the ALU issues in 72 % of the cycles.
+// Rows straight from memory to registers instead of through LDS: 548 us.
 #include "attn_common.h"
 #include "../../include/calvo.h"
 
@@ -288,6 +293,8 @@ __global__ void __launch_bounds__(64) mass_add_kernel(MassParams p, const MassAd
   p.mass_out[at] = x + before;
 }
 
+// K of a wave's tile in at most 64 registers, so that three waves share a SIMD.  0+8192 tokens (bf16, D = 128) at 8, 6, 5, 4, 3, 2 blocks of keys:
+// 352, 345, 322, 320, 324, 361 us; single tokens of 8 requests 44.6, 45.4, 44.7, 40.0, 41.3, 44.4.
 template <typename F>
 auto with_cfg(int dtype, int head_dim, F&& f) {
   if (dtype == CALVO_F32) {

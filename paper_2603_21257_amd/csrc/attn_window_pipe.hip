@@ -1,4 +1,9 @@
-// Attention with a window and first tokens on the pipelined bodies (attn_pipeline.h): bf16, 128-wide heads.
+// Attention with a window and first tokens on the pipelined bodies (attn_pipeline.h): bf16, 128-wide heads.  A tile's list of sub-tiles has
+// those in front that all its rows see, which the steady loop runs without a mask; the others (where windows begin, the diagonal, first tokens that end
+// inside a sub-tile) are met behind it one by one (WinPipeCfg).
+// Power bounds long launches, as it does the causal ones, and what is outside the steady loop: 14 us of a workgroup's start, masked sub-tiles and end.
+// 32Q/8KV: 0+32768 tokens behind 4096 1666 us, 1270 TFLOP/s of the pairs that are seen; 16384+2048 behind 4096 (one workgroup per CU) 122 us, 1130;
+// 28096+28, 28304+61 and 38304+209 behind 8192 (60 pieces of 128 rows) 49.5 us and 8 of merging.
 #include "attn_merge.h"
 #include "attn_pipeline.h"
 

@@ -9,7 +9,8 @@
 // of the range that there is, not of the leading bits: those of weights are few, and lanes that count on one word wait for each other.
 // Then one exchange of counts tells every wave where its kept tokens go.  256 rows of 16384 tokens: 20 us (bins of the leading eight bits 27;
 // the rank found bit by bit, tokens counted in the waves' masks, 37).
-// Move: one workgroup per destination block, bytes in, bytes out, at the rate of a large copy.
+// Move: one workgroup per destination block, bytes in, bytes out, at the rate of a large copy (32 layers of 8 heads, 2048 tokens each, bf16 D = 128: 113 us,
+// 4.75 TB/s of reads and writes).
 #include <cstring>
 #include <type_traits>
 
