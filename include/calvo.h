@@ -300,7 +300,7 @@ typedef struct {
  * calvo_window_destroy does not wait: the buffer is used again behind the launches that were queued.  A plan whose
  * calls were captured must outlive the graph's last replay.  It must precede calvo_destroy of its context.
  * Errors (nothing queued): CALVO_EINVAL for NULL pointers, negative counts, window < 1, slot ids outside the pool, repeated inside a request, or
- * that take new tokens and are in another request's table, more than 2^31 - 65537 tokens in a request, on a stream that is being captured;
+ * that take new tokens and are in another request's table, more than 2^31 - 65537 tokens in a request, more new tokens than a launch holds, on a stream that is being captured;
  * CALVO_ENOMEM if a request needs more slots than the pool has or a buffer cannot be had. */
 typedef struct calvo_window calvo_window;
 int calvo_window_prepare(calvo_ctx* ctx, const calvo_window_request* reqs, int n_reqs, int32_t window, int32_t n_first, calvo_window** out);
@@ -350,7 +350,7 @@ typedef struct {
  * slots can be given back (calvo_pool_release) once the compute stream has passed the call: loads run on streams of their own.
  * Queued on the compute stream; returns at once; cannot be captured.  Errors (nothing queued): CALVO_EINVAL for a bad layer range, NULL or misaligned
  * pointers, counts outside the limits above, slot ids outside the pool or repeated, strides below a request's tokens, buffers that overlap, more
- * than 65535 requests or layers; CALVO_ENOMEM if a request needs more slots than the pool has or a buffer cannot be had. */
+ * than 65535 requests or layers, 2^22 - 1 rows of weights (layer, request, KV head) or 2^28 - 16 kept tokens of a request; CALVO_ENOMEM if a request needs more slots than the pool has or a buffer cannot be had. */
 int calvo_kv_evict(calvo_ctx* ctx, const calvo_evict_request* reqs, int n_reqs, int layer_begin, int layer_end, const float* mass, int32_t mass_rows,
                    int64_t mass_stride, int32_t* kept, int64_t kept_stride, float* mass_out, int64_t out_stride);
 

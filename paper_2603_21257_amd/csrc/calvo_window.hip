@@ -165,6 +165,7 @@ int apart(const Range& a, const Range& b) {
 float scale_of(const calvo_ctx* c, float scale) { return scale > 0.f ? scale : 1.0f / sqrtf((float)c->cfg.head_dim); }
 
 constexpr int64_t kMostTokens = INT32_MAX - 65536;     // positions and their sums with tile sizes stay within 32 bits
+constexpr int64_t kMostThreads = UINT32_MAX;           // of a launch
 
 int check_window_requests(const calvo_config& cf, SlotMarks& marks, const calvo_window_request* reqs, int n_reqs, int32_t window, int32_t n_first,
                           int64_t* total) {
@@ -275,10 +276,10 @@ int window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, i
   if (w->mass_rows_differ)                // else calvo_attn_mass refuses the plan
     plan_mass(cf.n_q_heads / cf.n_kv_heads, cf.n_kv_heads, c->n_cus, tile_keys, lens, window, n_first, w->mass);
   const size_t n_mass = w->mass.items.size();
-  if ((int64_t)n_mass * cf.n_kv_heads > INT32_MAX) return fail(CALVO_EINVAL, "too many tokens in the batch");
+  if ((int64_t)n_mass * cf.n_kv_heads * std::max(256, tile_keys) > kMostThreads) return fail(CALVO_EINVAL, "too many tokens in the batch");
   const bool rows = w->plan.variant == kWindowRows;
   const size_t n_items = w->plan.items.size();
-  if ((int64_t)n_items * cf.n_q_heads > INT32_MAX) return fail(CALVO_EINVAL, "too many new tokens");
+  if ((int64_t)n_items * (rows ? cf.n_kv_heads : cf.n_q_heads / w->plan.heads_per_wg) * 512 > kMostThreads) return fail(CALVO_EINVAL, "too many new tokens");
 
   // ---- words: work items, first items of cut tiles, the same of the gathered weights, requests for the append, tables; pipelined kernels: the blocks'
   // offsets in a layer, even blocks first, padded as in the causal batches (kTablePad)
@@ -483,7 +484,8 @@ int kv_evict(calvo_ctx* c, const calvo_evict_request* reqs, int n_reqs, int laye
     for (const Range& a : x)
       for (const Range& b : x)
         if (&a < &b && (rc = apart(a, b)) != CALVO_OK) return rc;
-    if ((int64_t)n_layers * n_reqs * cf.n_kv_heads > INT32_MAX) return fail(CALVO_EINVAL, "too many requests and layers in a call");
+    if ((int64_t)n_layers * n_reqs * cf.n_kv_heads * 1024 > kMostThreads || blocks_of(max_keep) * 256 > kMostThreads)
+      return fail(CALVO_EINVAL, "too many requests, layers or kept tokens in a call");
   }
   ON_DEVICE(c);
   if (capturing(c)) return fail(CALVO_EINVAL, "calvo_kv_evict cannot be captured: its tables are read from the host");

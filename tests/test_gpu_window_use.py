@@ -346,3 +346,43 @@ def test_empty_batches():
         cb.calvo_kv_evict(ctx, [cb.make_evict_request([], 0, [], 0)], 0, 1, None, 0, 0, None, 0)
     finally:
         cb.calvo_destroy(ctx)
+
+
+def test_more_rows_of_weights_than_a_launch_holds():
+    """64 layers x 1025 requests x 64 heads; refused before anything is queued."""
+    layers, n, heads = 64, 1025, 64
+    pool = torch.empty((layers, 2 * n, 2, 16, heads, 8), dtype=torch.bfloat16, device=DEV)
+    mass = torch.full((layers, n, heads, 1), 7.0, device=DEV)
+    kept = torch.full((layers, n, heads, 1), 7, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    ctx = cb.calvo_create(layers, heads, heads, 8, cb.CALVO_BF16, 2 * n, pool)
+    try:
+        reqs = [cb.make_evict_request([r], 1, [n + r], 1, mass_row=r) for r in range(n)]
+        with pytest.raises(cb.CalvoError, match="too many"):
+            cb.calvo_kv_evict(ctx, reqs, 0, layers, mass, n, 1, kept, 1)
+        cb.calvo_kv_evict(ctx, reqs, 0, 2, mass, n, 1, kept, 1)
+        torch.cuda.synchronize()
+    finally:
+        cb.calvo_destroy(ctx)
+    assert bool((kept[:2] == 0).all()) and bool((kept[2:] == 7).all())
+
+
+def test_a_plan_that_is_not_weighed():
+    """mass_row -1: attention as ever, calvo_attn_mass refused."""
+    c = Case([(40, 9), (70, 1)], 8, 2, 64, seed=73)
+    want = c.run(30, 2)
+    pool, q, k, v = (x.to(DEV) for x in (c.pool, c.q, c.k, c.v))
+    out, lse, mass = torch.empty_like(q), torch.empty(q.shape[:-1], device=DEV), torch.full((1, 2, 2, 80), 7.0, device=DEV)
+    torch.cuda.synchronize()
+    ctx = c.create(pool)
+    try:
+        plan = cb.calvo_window_prepare(ctx, [cb.make_window_request(t, a, n, -1) for t, (a, n) in zip(c.tables, c.lens)], 30, 2)
+        cb.calvo_window_attn(plan, 0, q[0], k[0], v[0], out[0], lse[0])
+        with pytest.raises(cb.CalvoError, match="mass_row"):
+            cb.calvo_attn_mass(plan, 0, q[0], lse[0], None, mass[0], 2, 80)
+        cb.calvo_window_destroy(plan)
+        torch.cuda.synchronize()
+    finally:
+        cb.calvo_destroy(ctx)
+    assert torch.equal(out.cpu().view(torch.int16), want["out"].view(torch.int16)) and torch.equal(lse.cpu(), want["lse"])
+    assert bool((mass == 7).all())
