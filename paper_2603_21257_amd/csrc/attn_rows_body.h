@@ -97,6 +97,99 @@ __device__ inline unsigned bf16_rne(float x) {
 }
 __device__ inline float bf16_widen(unsigned b) { return __builtin_bit_cast(float, b << 16); }
 
+// Partial results that other workgroups of the launch read: relaxed atomics of the device's scope go through the caches of an XCD to where all of them
+// meet, and are there when they have been waited for.
+__device__ inline void store_through(float* a, float x, float y) {
+  __hip_atomic_store((unsigned long long*)a, __builtin_bit_cast(unsigned long long, (f32x2){x, y}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline f32x2 load_through(const float* a) {
+  return __builtin_bit_cast(f32x2, __hip_atomic_load((const unsigned long long*)a, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// One row of a cut tile, one wave: its n pieces from work item `first` on.  SAME: they come from this launch, and no load of theirs stands in a condition
+// (32Q/4KV, D = 128, 20000+1 tokens in four requests 19.6 / 18.8 us a call).
+template <typename T, int DP, int ROWS, bool SAME, typename P>
+__device__ inline void merge_row(const P& p, int first, int n, int kv, int row, unsigned rho, int q_off) {
+  constexpr bool WIN = std::is_same<P, WinParams>::value;
+  constexpr int W = DP / 64;                                   // consecutive floats of a lane
+  typedef typename std::conditional<W == 4, f32x4, typename std::conditional<W == 2, f32x2, float>::type>::type vec;
+  const int lane = threadIdx.x & 63;
+  const int Hkv = p.n_kv_heads, Hq = p.n_q_heads, D = p.head_dim;
+  const unsigned G = p.group;
+  const int64_t base = ((int64_t)first * Hkv + kv) * ROWS + row;
+  const int64_t step = (int64_t)Hkv * ROWS;
+  const f32x2* ml = (const f32x2*)p.part_ml + base;
+  const float* po = p.part_o + base * DP + W * lane;
+  // at most 64 pieces per tile (attn_plan.cpp): lane i holds piece i
+  f32x2 mine = {-INFINITY, 0.f};
+  if (lane < n) {
+    if constexpr (SAME) mine = load_through((const float*)(ml + lane * step));
+    else mine = ml[lane * step];
+  }
+  constexpr int B = W > 2 ? 8 : 16 / W;                        // loads in flight: the first are on their way while the weights are found
+  vec v[B];
+  // Past the end nothing, or the last piece again where that costs no more than the branch: 4 bytes a lane, or one wave of a CU
+  auto fetch = [&](int c0) {
+#pragma unroll
+    for (int i = 0; i < B; i++)
+      if (W == 1 || SAME || c0 + i < n) {
+        const float* a = po + min(c0 + i, n - 1) * step * DP;
+        if constexpr (!SAME) v[i] = *(const vec*)a;
+        else if constexpr (W == 1) v[i] = __hip_atomic_load(a, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        else if constexpr (W == 2) v[i] = load_through(a);
+        else {
+          const f32x2 x = load_through(a), y = load_through(a + 2);
+          v[i] = (vec){x[0], x[1], y[0], y[1]};
+        }
+      }
+  };
+  fetch(0);
+  __builtin_amdgcn_sched_barrier(0);
+  float all = mine[0];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor(all, o));
+  const float wgt = mine[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine[0] - all);
+  float l = wgt * mine[1];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o);
+  float acc[W];
+#pragma unroll
+  for (int e = 0; e < W; e++) acc[e] = 0.f;
+  for (int c0 = 0; c0 < n; c0 += B) {
+    if (c0) fetch(c0);
+#pragma unroll
+    for (int i = 0; i < B; i++) {
+      if (c0 + i >= n) break;
+      const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wgt), c0 + i));
+#pragma unroll
+      for (int e = 0; e < W; e++) {
+        float x;
+        if constexpr (W == 1) x = v[i];
+        else x = v[i][e];
+        acc[e] = __builtin_fmaf(w, x, acc[e]);
+      }
+    }
+  }
+  auto qrow = [&] {
+    const unsigned tok = rho / G;
+    return (int64_t)(q_off + (int)tok) * Hq + kv * (int)G + (int)(rho - tok * G);
+  };
+  if constexpr (!WIN) {
+    if (threadIdx.x == 0) clock_end_tail(p.clock.words);
+  } else {
+    if (p.lse && lane == 0) p.lse[qrow()] = log_sum(all, l);
+  }
+  const int d = W * lane;
+  if (d >= D) return;
+  const float inv = 1.f / l;
+  T* out = (T*)p.out + qrow() * D + d;
+#pragma unroll
+  for (int e = 0; e < W; e++) {
+    if constexpr (sizeof(T) == 4) out[e] = acc[e] * inv;
+    else out[e] = (T)bf16_rne(acc[e] * inv);
+  }
+}
+
 template <class C>
 __global__ void __launch_bounds__(64 * C::NW) attn_rows_kernel(typename C::Params p) {
   typedef typename C::T T;
@@ -126,13 +219,14 @@ __global__ void __launch_bounds__(64 * C::NW) attn_rows_kernel(typename C::Param
   }
   constexpr int SPS = 2 / KB;                                  // steps per 32-key sub-tile
   int tile, sub_begin = 0, sub_end, n_splits = 1;
-  int first_steps = 0, gap = 0;                                // WIN: steps over first tokens, steps left out behind them
+  int first_steps = 0, gap = 0, first_item = 0;                // WIN: steps over first tokens, steps left out behind them
   bool first_piece = true;
   ReqDesc rd;
   if constexpr (!WIN) rd = p.one;                              // a batch of one request comes with the launch
   if constexpr (WIN) {
     const WinItem wi = load_win_item(p.items, it);
     tile = wi.q_tile; sub_begin = wi.sub_begin; sub_end = wi.sub_end; n_splits = wi.n_splits;
+    first_item = wi.first_item;
     first_steps = wi.first_subs * SPS;
     gap = wi.gap * SPS;
     rd = {wi.table_off, wi.n_cached, wi.n_new, wi.q_off};
@@ -680,12 +774,18 @@ __global__ void __launch_bounds__(64 * C::NW) attn_rows_kernel(typename C::Param
     }
   }
   const int64_t part = (int64_t)it * Hkv + kv;
+  bool along = false;                                          // WIN: the tile's last piece merges them
+  if constexpr (WIN) along = p.arrived != nullptr;
   if (n_splits > 1 && wave == 0 && g == 0) {
 #pragma unroll
     for (int qb = 0; qb < NQB; qb++) {
       float* pm = p.part_ml + (part * C::ROWS + 16 * qb + c) * 2;
-      pm[0] = m[qb];
-      pm[1] = l[qb];
+      if (along) {
+        store_through(pm, m[qb], l[qb]);
+      } else {
+        pm[0] = m[qb];
+        pm[1] = l[qb];
+      }
     }
   }
 #pragma unroll
@@ -712,7 +812,14 @@ __global__ void __launch_bounds__(64 * C::NW) attn_rows_kernel(typename C::Param
         if (n_splits > 1) {
           float* po = p.part_o + (part * C::ROWS + 16 * qb + c) * DP + d;
 #pragma unroll
-          for (int e = 0; e < VW; e += 4) *(f32x4*)(po + e) = (f32x4){x[e], x[e + 1], x[e + 2], x[e + 3]};
+          for (int e = 0; e < VW; e += 4) {
+            if (!along) {
+              *(f32x4*)(po + e) = (f32x4){x[e], x[e + 1], x[e + 2], x[e + 3]};
+            } else if (ok[qb]) {
+              store_through(po + e, x[e], x[e + 1]);
+              store_through(po + e + 2, x[e + 2], x[e + 3]);
+            }
+          }
         } else if (ok[qb] && (C::FULL || d < D)) {
           const float inv = 1.f / l[qb];
           T* po = (T*)p.out + qrow[qb] * D + d;
@@ -728,6 +835,22 @@ __global__ void __launch_bounds__(64 * C::NW) attn_rows_kernel(typename C::Param
       }
   if constexpr (!WIN) {
     if (threadIdx.x == 0) clock_end(p.clock.words);
+  } else if (along && n_splits > 1) {
+    // Few rows: a merge launch costs more than what it does.  The piece that finds all others counted merges them, in their order, and leaves a zero for the
+    // next launch.  No fence of the device's scope: it would write an L2 back for every piece (4096+1 tokens behind 1024, 32Q/8KV: 17.3 us a call with fences,
+    // 10.9 with the merge as a launch, 8.9 this way).
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    __syncthreads();                                           // every wave's; and LDS is free
+    if (threadIdx.x == 0) {
+      int32_t* const count = p.arrived + (int64_t)first_item * Hkv + kv;
+      const int before = __hip_atomic_fetch_add(count, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (before == n_splits - 1) __hip_atomic_store(count, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      *(int32_t*)smem = before;
+    }
+    __syncthreads();
+    if (*(const int32_t*)smem != n_splits - 1) return;
+    const int here = (int)min(RT, n_rows - row0);
+    for (int row = wave; row < here; row += NW) merge_row<T, DP, C::ROWS, true>(p, first_item, n_splits, kv, row, row0 + row, rd.q_off);
   }
 }
 
@@ -739,12 +862,8 @@ __global__ void __launch_bounds__(64 * C::NW) attn_rows_kernel(typename C::Param
 template <typename T, int DP, int ROWS, typename P = RowsParams>
 __global__ void __launch_bounds__(256) merge_rows_kernel(P p, const int32_t* split_tiles) {
   constexpr bool WIN = std::is_same<P, WinParams>::value;
-  constexpr int W = DP / 64;                                   // consecutive floats of a lane
-  typedef typename std::conditional<W == 4, f32x4, typename std::conditional<W == 2, f32x2, float>::type>::type vec;
-  const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int Hkv = p.n_kv_heads, Hq = p.n_q_heads, D = p.head_dim;
-  const unsigned G = p.group;
+  const int Hkv = p.n_kv_heads;
   const int row = (blockIdx.x % (ROWS / 4)) * 4 + wave;
   const int slot_id = blockIdx.x / (ROWS / 4), kv = slot_id % Hkv, first = ((const_i32p)(uintptr_t)split_tiles)[slot_id / Hkv];
   int q_tile, suffix_len, q_off, n;
@@ -756,66 +875,8 @@ __global__ void __launch_bounds__(256) merge_rows_kernel(P p, const int32_t* spl
     q_tile = wi.q_tile; suffix_len = wi.suffix_len; q_off = wi.q_off; n = wi.n_splits;
   }
   const unsigned rho = (unsigned)q_tile * ROWS + row;
-  if (rho >= (unsigned)suffix_len * G) return;
-  const int64_t base = ((int64_t)first * Hkv + kv) * ROWS + row;
-  const int64_t step = (int64_t)Hkv * ROWS;
-  const f32x2* ml = (const f32x2*)p.part_ml + base;
-  const float* po = p.part_o + base * DP + W * lane;
-  // at most 64 pieces per tile (attn_plan.cpp): lane i holds piece i
-  const f32x2 mine = lane < n ? ml[lane * step] : (f32x2){-INFINITY, 0.f};
-  constexpr int B = W > 2 ? 8 : 16 / W;                        // loads in flight: the first are on their way while the weights are found
-  vec v[B];
-  // Past the end nothing, or (4 bytes a lane) the last piece again, which costs no more than the branch
-  auto fetch = [&](int c0) {
-#pragma unroll
-    for (int i = 0; i < B; i++)
-      if (W == 1 || c0 + i < n) v[i] = *(const vec*)(po + min(c0 + i, n - 1) * step * DP);
-  };
-  fetch(0);
-  __builtin_amdgcn_sched_barrier(0);
-  float all = mine[0];
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor(all, o));
-  const float wgt = mine[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine[0] - all);
-  float l = wgt * mine[1];
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o);
-  float acc[W];
-#pragma unroll
-  for (int e = 0; e < W; e++) acc[e] = 0.f;
-  for (int c0 = 0; c0 < n; c0 += B) {
-    if (c0) fetch(c0);
-#pragma unroll
-    for (int i = 0; i < B; i++) {
-      if (c0 + i >= n) break;
-      const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wgt), c0 + i));
-#pragma unroll
-      for (int e = 0; e < W; e++) {
-        float x;
-        if constexpr (W == 1) x = v[i];
-        else x = v[i][e];
-        acc[e] = __builtin_fmaf(w, x, acc[e]);
-      }
-    }
-  }
-  auto qrow = [&] {
-    const unsigned tok = rho / G;
-    return (int64_t)(q_off + (int)tok) * Hq + kv * (int)G + (int)(rho - tok * G);
-  };
-  if constexpr (!WIN) {
-    if (threadIdx.x == 0) clock_end_tail(p.clock.words);
-  } else {
-    if (p.lse && lane == 0) p.lse[qrow()] = log_sum(all, l);
-  }
-  const int d = W * lane;
-  if (d >= D) return;
-  const float inv = 1.f / l;
-  T* out = (T*)p.out + qrow() * D + d;
-#pragma unroll
-  for (int e = 0; e < W; e++) {
-    if constexpr (sizeof(T) == 4) out[e] = acc[e] * inv;
-    else out[e] = (T)bf16_rne(acc[e] * inv);
-  }
+  if (rho >= (unsigned)suffix_len * p.group) return;
+  merge_row<T, DP, ROWS, false>(p, first, n, kv, row, rho, q_off);
 }
 
 }  // namespace rows

@@ -152,6 +152,7 @@ struct WinParams {
   float scale;
   float* part_o;             // partial results of cut tiles as in RowsParams
   float* part_ml;
+  int32_t* arrived;          // packed rows: pieces of a tile that are done, [first item][KV head], and the last one merges them; or NULL: a launch behind does
 };
 // raises the kernels' dynamic LDS limit; before the first launch on a device
 hipError_t attn_window_prepare(int dtype, int head_dim, int tile_rows);

@@ -24,7 +24,7 @@ struct calvo_window {
   MassPlan mass;
   StepBuf buf;
   // 32-bit words from the beginning of buf.d
-  size_t items_at = 0, split_at = 0, mass_at = 0, add_at = 0, append_at = 0, tables_at = 0, offs_at = 0;
+  size_t items_at = 0, split_at = 0, arrived_at = 0, mass_at = 0, add_at = 0, append_at = 0, tables_at = 0, offs_at = 0;
   size_t part_o_at = 0, part_ml_at = 0, part_mass_at = 0; // floats, behind them
 };
 
@@ -287,7 +287,9 @@ int window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, i
   auto pad4 = [](size_t n) { return (n + 3) / 4 * 4; };
   w->items_at = 0;
   w->split_at = n_items * kItem;
-  w->mass_at = pad4(w->split_at + w->plan.split_tiles.size());
+  w->arrived_at = w->split_at + w->plan.split_tiles.size();
+  const size_t n_arrived = w->plan.one_launch ? n_items * (size_t)cf.n_kv_heads : 0;
+  w->mass_at = pad4(w->arrived_at + n_arrived);
   w->add_at = w->mass_at + n_mass * kMass;
   w->append_at = w->add_at + w->mass.adds.size() * kAdd;
   w->tables_at = w->append_at + (size_t)n_reqs * kApp;
@@ -343,6 +345,7 @@ int window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, i
     const MassAdd d = {reqs[x.req].n_cached, reqs[x.req].n_cached + reqs[x.req].n_new, reqs[x.req].mass_row, x.tile, x.part, x.n_parts, {0, 0}};
     memcpy(h + w->add_at + i * kAdd, &d, sizeof d);
   }
+  std::fill_n(h + w->arrived_at, n_arrived, 0);
   if (!w->plan.split_tiles.empty()) memcpy(h + w->split_at, w->plan.split_tiles.data(), w->plan.split_tiles.size() * 4);
   return upload(c, w->buf, words);
 }
@@ -403,7 +406,8 @@ int window_attn(calvo_window* w, int layer, const void* q, const void* k_new, co
   p.part_o = (float*)d + w->part_o_at; p.part_ml = (float*)d + w->part_ml_at;
   const int n_items = (int)w->plan.items.size(), n_cut = (int)w->plan.split_tiles.size();
   if (w->plan.variant == kWindowRows) {
-    HIP_TRY(launch_attn_window(p, cf.dtype, w->plan.tile_rows, n_items, d + w->split_at, n_cut, c->s_compute));
+    if (w->plan.one_launch) p.arrived = w->buf.d + w->arrived_at;
+    HIP_TRY(launch_attn_window(p, cf.dtype, w->plan.tile_rows, n_items, d + w->split_at, p.arrived ? 0 : n_cut, c->s_compute));
   } else {
     p.heads_per_wg = w->plan.heads_per_wg;
     p.row_blocks_per_wg = attn_mfma_row_blocks(w->plan.variant);

@@ -152,6 +152,12 @@ void plan_window(const WindowShape& s, const std::vector<WindowLens>& lens, int3
     out.tile_rows = best.shape.tile_rows;
     out.single_tiles = true;
     for (const WindowLens& l : lens) out.single_tiles &= (int64_t)l.n_new * group <= best.shape.tile_rows;
+    // At most one row for each wave of a workgroup: then the last piece of a tile merges them (attn_rows_body.h).  us a call of one caller, by a launch
+    // behind / by the last piece: bf16 D = 128, 32Q/8KV, 4096+1 behind 1024 10.9 / 8.9, four such requests 11.5 / 9.2, 64Q/8KV 12.4 / 12.3 behind 4096; 32Q/4KV
+    // 11.6 / 12.0; D = 64, 16Q/4KV 11.6 / 9.6; D = 256, 16Q/4KV 14.4 / 14.5, 8Q/8KV 15.0 / 14.7; fp32 D = 128, 32Q/8KV 15.0 / 14.8, 32Q/4KV 13.9 / 14.0.  Two rows
+    // a wave and more: 64Q/4KV 12.5 / 16.9, 16Q/1KV 11.7 / 15.9, D = 256 32Q/4KV 14.4 / 20.4, 64Q/4KV 15.1 / 30.4.
+    out.one_launch = out.single_tiles && best.shape.tile_rows == kFewRows;
+    for (const WindowLens& l : lens) out.one_launch &= (int64_t)l.n_new * group <= (s.head_dim <= 128 ? 8 : 4);
     out.part_rows = (int64_t)s.n_kv_heads * best.shape.tile_rows;
     out.part_width = s.head_dim <= 64 ? 64 : s.head_dim <= 128 ? 128 : 256;
   } else {

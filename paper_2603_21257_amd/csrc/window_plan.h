@@ -35,6 +35,7 @@ struct WindowPlan {
   int tile_tokens = 0;                   // pipelined: tokens of a tile
   int heads_per_wg = 1;                  // pipelined
   bool single_tiles = false;             // packed rows: no request has more than one tile
+  bool one_launch = false;               // single_tiles with at most one row for each wave of a workgroup
   int64_t part_rows = 0, part_width = 0; // rows of partial results that a work item leaves over all heads, floats of one
   std::vector<WindowPiece> items;
   std::vector<int32_t> split_tiles;      // first item of every cut tile

@@ -386,3 +386,41 @@ def test_a_plan_that_is_not_weighed():
         cb.calvo_destroy(ctx)
     assert torch.equal(out.cpu().view(torch.int16), want["out"].view(torch.int16)) and torch.equal(lse.cpu(), want["lse"])
     assert bool((mass == 7).all())
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dim", [("bf16", 32, 8, 128), ("bf16", 8, 1, 64), ("bf16", 8, 2, 256), ("f32", 6, 3, 40), ("f32", 4, 1, 256), ("bf16", 16, 1, 128)])
+@pytest.mark.parametrize("pieces", ["2", "9", "64"])
+def test_single_tokens_in_pieces(dtype, hq, hkv, dim, pieces, monkeypatch):
+    """Eagerly and as a graph of three layers, replayed; the pieces of a tile arrive in any order and are merged in theirs: the same bits each time."""
+    monkeypatch.setenv("CALVO_ATTN_SPLITS", pieces)
+    c = Case([(3000, 1), (0, 1), (17, 1), (700, 0), (2111, 1)], hq, hkv, dim, dtype, seed=77, layers=3)
+    want = c.run(1500, 5)
+    wh.check_pool(c, want)
+    for l in range(3):
+        wh.check_attn(c, want, 1500, 5, l)
+    stream = torch.cuda.Stream()
+    pool, q, k, v = (x.to(DEV) for x in (c.pool, c.q, c.k, c.v))
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:-1], device=DEV)
+    torch.cuda.synchronize()
+    ctx = c.create(pool, stream.cuda_stream)
+    try:
+        plan = cb.calvo_window_prepare(ctx, c.requests(), 1500, 5)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            for l in range(3):
+                cb.calvo_window_attn(plan, l, q[l], k[l], v[l], out[l], lse[l])
+        for rep in range(20):
+            out.zero_()
+            lse.zero_()
+            torch.cuda.synchronize()
+            with torch.cuda.stream(stream):
+                graph.replay()
+            if rep % 5 == 4:
+                for l in range(3):
+                    cb.calvo_window_attn(plan, l, q[l], k[l], v[l], out[l], lse[l])
+            torch.cuda.synchronize()
+            assert torch.equal(out.cpu(), want["out"]) and torch.equal(lse.cpu(), want["lse"])
+        del graph
+        cb.calvo_window_destroy(plan)
+    finally:
+        cb.calvo_destroy(ctx)
