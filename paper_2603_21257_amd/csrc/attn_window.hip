@@ -1,7 +1,7 @@
 // Launches of the attention with a sliding window and first tokens that stay visible (calvo_window_attn), on packed rows
 // (attn_rows_body.h): every element type, head width and group size.
 // 32 requests of 300 to 33000 tokens, one new one each, 32Q/8KV behind 4096: 75 us, 4.6 TB/s of K and V, bound by those reads.  One such request
-// behind 1024: 6.6 us and 3.8 of merging, bound by the chain start, lookup, K, V, combination.  bf16 D = 64, 16Q/4KV, 4111+300 behind 2048: 17.3 us, one
+// behind 1024: 9 us, bound by the chain start, lookup, K, V, combination, merge of nine pieces.  bf16 D = 64, 16Q/4KV, 4111+300 behind 2048: 17.3 us, one
 // workgroup on each of 152 CUs; fp32 D = 64, 8Q/2KV, 1000+128 behind 300: 9.9 us.
 #include "attn_rows_body.h"
 
