@@ -273,7 +273,7 @@ int window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, i
   plan_window({cf.dtype == CALVO_F32, cf.head_dim, cf.n_q_heads, cf.n_kv_heads, c->n_cus, c->force_splits, c->force_rows_tile, forced_variant()}, lens,
               window, n_first, w->plan);
   const int tile_keys = attn_mass_tile_keys(cf.dtype, cf.head_dim);
-  if (w->mass_rows_differ)                // else calvo_attn_mass refuses the plan
+  if (w->mass_rows_differ)                // else calvo_attn_mass refuses the plan (32 requests of 300 to 33000 tokens: 28 us with it, 21 without)
     plan_mass(cf.n_q_heads / cf.n_kv_heads, cf.n_kv_heads, c->n_cus, tile_keys, lens, window, n_first, w->mass);
   const size_t n_mass = w->mass.items.size();
   if ((int64_t)n_mass * cf.n_kv_heads * std::max(256, tile_keys) > kMostThreads) return fail(CALVO_EINVAL, "too many tokens in the batch");
