@@ -76,13 +76,19 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(EvictParams p, W
   const bool stays = steps <= V;
   // a lane's ranks: kSafe of a token that stays anyway, kNobody past the end
   uint32_t x[V];
-  // the weights themselves: a buffer of those that are there, past its end a load reads 0 without a branch
+  // the weights themselves: a buffer of those that are there, past its end a load reads 0 without a branch.  The step is in the vector offset, which is
+  // what is compared with the end; a scalar offset is not.
   auto read = [&](int s0, uint32_t (&w)[V]) {
     const int64_t at = (int64_t)wave * steps * 64 + 64 * s0;
     const int here = (int)max((int64_t)0, min((int64_t)n - at, (int64_t)64 * min(V, steps - s0)));
     const auto buf = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(mass + min(at, (int64_t)n)), 0, 4 * here, 0x00020000u);
 #pragma unroll
-    for (int j = 0; j < V; j++) w[j] = __builtin_amdgcn_raw_buffer_load_b32(buf, 4 * lane, 256 * j, 0);
+    for (int j0 = 0; j0 < V; j0 += 16) {
+      int off = 4 * lane + 256 * j0;                           // one for 16 steps, the rest is immediate: of its own each takes a register
+      asm volatile("" : "+v"(off));
+#pragma unroll
+      for (int j = j0; j < min(V, j0 + 16); j++) w[j] = __builtin_amdgcn_raw_buffer_load_b32(buf, off + 256 * (j - j0), 0, 0);
+    }
   };
   auto load = [&](int s0) {
     read(s0, x);
