@@ -297,8 +297,9 @@ typedef struct {
 /* Checks, plans and describes a batch to the device once, for all layers of a step (the upload is queued on the compute stream).
  * window >= 1 (INT32_MAX hides nothing), n_first >= 0.  Descriptors and the partial results of cut tiles are in a buffer of the plan's own,
  * so that launches and captured graphs of different plans do not meet; those of one plan must not run at the same time.
- * calvo_window_destroy does not wait: the buffer is used again behind the launches that were queued.  A plan whose
- * calls were captured must outlive the graph's last replay.  It must precede calvo_destroy of its context.
+ * calvo_window_destroy does not wait: the buffer is used again behind the launches that were queued, by plans that it is large enough for.  A
+ * prepare for which none is makes one, and may wait for the device there (sizes go up in powers of two).  A plan whose calls were captured must
+ * outlive the graph's last replay.  It must precede calvo_destroy of its context.
  * Errors (nothing queued): CALVO_EINVAL for NULL pointers, negative counts, window < 1, slot ids outside the pool, repeated inside a request, or
  * that take new tokens and are in another request's table, more than 2^31 - 65537 tokens in a request, more new tokens than a launch holds, on a stream that is being captured;
  * CALVO_ENOMEM if a request needs more slots than the pool has or a buffer cannot be had. */
@@ -348,7 +349,7 @@ typedef struct {
  * mass: DEVICE fp32 [layers][mass_rows][Hkv][mass_stride]; mass_out the same with out_stride; kept: DEVICE int32
  * [layers][n_reqs][Hkv][kept_stride].  Nothing else is written.  With dst_table the request goes on as one of n_keep cached tokens, and the source
  * slots can be given back (calvo_pool_release) once the compute stream has passed the call: loads run on streams of their own.
- * Queued on the compute stream; returns at once; cannot be captured.  Errors (nothing queued): CALVO_EINVAL for a bad layer range, NULL or misaligned
+ * Queued on the compute stream; returns at once (a buffer for larger tables than before is made as in calvo_window_prepare); cannot be captured.  Errors (nothing queued): CALVO_EINVAL for a bad layer range, NULL or misaligned
  * pointers, counts outside the limits above, slot ids outside the pool or repeated, strides below a request's tokens, buffers that overlap, more
  * than 65535 requests or layers, 2^22 - 1 rows of weights (layer, request, KV head) or 2^28 - 16 kept tokens of a request; CALVO_ENOMEM if a request needs more slots than the pool has or a buffer cannot be had. */
 int calvo_kv_evict(calvo_ctx* ctx, const calvo_evict_request* reqs, int n_reqs, int layer_begin, int layer_end, const float* mass, int32_t mass_rows,

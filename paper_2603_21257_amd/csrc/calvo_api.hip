@@ -123,7 +123,10 @@ void destroy_partial(calvo_ctx* c) {
   if (c->part_o) (void)hipFree(c->part_o);
   if (c->part_ml) (void)hipFree(c->part_ml);
   for (auto& b : c->blob_free) { (void)hipFree(b.d); (void)hipHostFree(b.h); }
-  for (auto& b : c->step_free) { (void)hipFree(b.d); (void)hipHostFree(b.h); (void)hipEventDestroy(b.read); }
+  struct {
+    void free(StepBuf& b) { (void)hipFree(b.d); (void)hipHostFree(b.h); (void)hipEventDestroy(b.read); }
+  } step_dev;
+  c->step_bufs.clear(step_dev);
   for (auto& s : c->s_copy) if (s) (void)hipStreamDestroy(s);
   if (c->s_scatter) (void)hipStreamDestroy(c->s_scatter);
   if (c->own_compute && c->s_compute) (void)hipStreamDestroy(c->s_compute);

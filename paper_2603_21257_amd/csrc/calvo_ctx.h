@@ -12,6 +12,7 @@
 
 #include "../../include/calvo.h"
 #include "calvo_internal.h"
+#include "step_bufs.h"
 
 namespace calvo {
 // Descriptors and partial results of one batch or call (calvo_window.hip): device memory, its pinned source, and the event behind the
@@ -123,7 +124,7 @@ struct calvo_ctx {
   struct BlobBuf { int32_t* d; int32_t* h; size_t bytes; };
   std::mutex blob_mu;
   std::vector<BlobBuf> blob_free;
-  std::vector<calvo::StepBuf> step_free;      // of calvo_window.hip, given back (guarded by blob_mu)
+  calvo::StepBufs<calvo::StepBuf> step_bufs;  // of calvo_window.hip, given back
   calvo::SlotMarks marks;
   bool window_kernels = false;               // their LDS limits are raised
   std::vector<void*> l2_ring;

@@ -57,65 +57,47 @@ bool capturing(calvo_ctx* c) {
   return s != hipStreamCaptureStatusNone;
 }
 
-// ---- descriptor buffers.  One that is given back is used again behind the launches that read it, on the same stream, so nobody waits for
-// them; only its pinned source must have been read before it is written again.  A few are kept in turn, so that a program that is some steps
-// ahead of the device finds one that has been.
+// ---- descriptor buffers (step_bufs.h)
+struct StepDev {
+  calvo_ctx* c;
+  int make(StepBuf& b) {
+    HIP_TRY(hipMalloc((void**)&b.d, b.d_bytes));
+    HIP_TRY(hipHostMalloc((void**)&b.h, b.h_bytes, hipHostMallocMapped | hipHostMallocCoherent));
+    HIP_TRY(hipEventCreateWithFlags(&b.read, hipEventDisableTiming));
+    return CALVO_OK;
+  }
+  // behind everything that was queued with it
+  void free(StepBuf& b) {
+    (void)hipStreamSynchronize(c->s_compute);
+    if (b.d) (void)hipFree(b.d);
+    if (b.h) (void)hipHostFree(b.h);
+    if (b.read) (void)hipEventDestroy(b.read);
+    (void)hipGetLastError();
+    b = StepBuf();
+  }
+  bool was_read(StepBuf& b) {
+    if (hipEventQuery(b.read) == hipSuccess) return true;
+    (void)hipGetLastError();
+    return false;
+  }
+  int wait(StepBuf& b) {
+    HIP_TRY(hipEventSynchronize(b.read));
+    return CALVO_OK;
+  }
+};
+
+// The caller gives the buffer back, also after an error.
 int take_buf(calvo_ctx* c, size_t d_bytes, size_t h_bytes, StepBuf& out) {
-  constexpr int kInTurn = 4;
-  {
-    std::lock_guard<std::mutex> lk(c->blob_mu);
-    int best = -1, fit = 0;
-    bool best_read = false;
-    for (int i = 0; i < (int)c->step_free.size(); i++) {
-      StepBuf& b = c->step_free[i];
-      if (b.d_bytes < d_bytes || b.h_bytes < h_bytes) continue;
-      fit++;
-      if (b.pending && !best_read) {
-        if (hipEventQuery(b.read) == hipSuccess) b.pending = false;
-        else (void)hipGetLastError();
-      }
-      const bool better = best < 0 || (!b.pending && !best_read) || (!b.pending && b.d_bytes < c->step_free[best].d_bytes);
-      if (better) { best = i; best_read = !b.pending; }
-    }
-    if (best >= 0 && (best_read || fit >= kInTurn)) {
-      out = c->step_free[best];
-      c->step_free.erase(c->step_free.begin() + best);
-    }
-  }
-  if (!out.d) {
-    out.d_bytes = (d_bytes + 65535) / 65536 * 65536;
-    out.h_bytes = (h_bytes + 16383) / 16384 * 16384;
-    HIP_TRY(hipMalloc((void**)&out.d, out.d_bytes));
-    HIP_TRY(hipHostMalloc((void**)&out.h, out.h_bytes, hipHostMallocMapped | hipHostMallocCoherent));
-    HIP_TRY(hipEventCreateWithFlags(&out.read, hipEventDisableTiming));
-  }
-  if (out.pending) {
-    HIP_TRY(hipEventSynchronize(out.read));
-    out.pending = false;
-  }
-  return CALVO_OK;
+  StepDev dev{c};
+  return c->step_bufs.take(dev, d_bytes, h_bytes, out);
 }
 
-void free_buf(StepBuf& b) {
-  if (b.d) (void)hipFree(b.d);
-  if (b.h) (void)hipHostFree(b.h);
-  if (b.read) (void)hipEventDestroy(b.read);
-  b = StepBuf();
+void free_buf(calvo_ctx* c, StepBuf& b) {
+  if (b.d || b.h || b.read) StepDev{c}.free(b);
 }
 
 void give_buf(calvo_ctx* c, StepBuf& b) {
-  constexpr size_t kKeep = 64;
-  if (b.d && b.h && b.read) {
-    std::lock_guard<std::mutex> lk(c->blob_mu);
-    if (c->step_free.size() < kKeep) {
-      try {
-        c->step_free.push_back(b);
-        b = StepBuf();
-        return;
-      } catch (const std::bad_alloc&) {}
-    }
-  }
-  free_buf(b);                          // hipFree waits for the device
+  if (!b.d || !b.h || !b.read || !c->step_bufs.give(b)) free_buf(c, b);
 }
 
 int upload(calvo_ctx* c, StepBuf& b, size_t words) {
@@ -502,7 +484,7 @@ int kv_evict(calvo_ctx* c, const calvo_evict_request* reqs, int n_reqs, int laye
   const bool in_args = words <= (size_t)kEvictArgWords;
   int32_t args[kEvictArgWords];
   StepBuf buf;
-  if (!in_args && (rc = take_buf(c, words * 4, words * 4, buf)) != CALVO_OK) { free_buf(buf); return rc; }
+  if (!in_args && (rc = take_buf(c, words * 4, words * 4, buf)) != CALVO_OK) { free_buf(c, buf); return rc; }
   int32_t* const h = in_args ? args : buf.h;
   int32_t at = 0;
   int32_t* tables = h + (size_t)n_reqs * kReq;
@@ -516,24 +498,22 @@ int kv_evict(calvo_ctx* c, const calvo_evict_request* reqs, int n_reqs, int laye
     at += ns + nd;
   }
   const int n_words = (int)((size_t)n_reqs * kReq) + at;
-  if (!in_args) rc = upload(c, buf, words);
-  if (rc == CALVO_OK) {
-    EvictParams p{};
-    p.pool = (unsigned char*)cf.pool + (int64_t)layer_begin * c->layer_bytes;
-    p.reqs = (const EvictDesc*)buf.d; p.tables = in_args ? nullptr : buf.d + (size_t)n_reqs * kReq;
-    p.mass = mass; p.mass_out = mass_out; p.kept = kept;
-    p.layer_bytes = c->layer_bytes;
-    p.mass_stride = mass_stride; p.mass_layer = (int64_t)mass_rows * cf.n_kv_heads * mass_stride;
-    p.out_stride = out_stride; p.out_layer = (int64_t)mass_rows * cf.n_kv_heads * out_stride;
-    p.kept_stride = kept_stride;
-    p.n_reqs = n_reqs; p.n_layers = n_layers; p.n_kv_heads = cf.n_kv_heads;
-    p.row_chunks = (int32_t)((size_t)cf.head_dim * c->elt / 16);
-    p.max_tokens = (int32_t)longest;
-    p.max_keep = max_keep;
-    hipError_t e = launch_evict_select(p, in_args ? args : nullptr, n_words, c->s_compute);
-    if (e == hipSuccess) e = launch_evict_move(p, in_args ? args : nullptr, n_words, c->s_compute);
-    if (e != hipSuccess) rc = fail_hip(e, "launch of calvo_kv_evict");
-  }
+  if (!in_args && (rc = upload(c, buf, words)) != CALVO_OK) { free_buf(c, buf); return rc; }   // it may be under way, without an event behind it
+  EvictParams p{};
+  p.pool = (unsigned char*)cf.pool + (int64_t)layer_begin * c->layer_bytes;
+  p.reqs = (const EvictDesc*)buf.d; p.tables = in_args ? nullptr : buf.d + (size_t)n_reqs * kReq;
+  p.mass = mass; p.mass_out = mass_out; p.kept = kept;
+  p.layer_bytes = c->layer_bytes;
+  p.mass_stride = mass_stride; p.mass_layer = (int64_t)mass_rows * cf.n_kv_heads * mass_stride;
+  p.out_stride = out_stride; p.out_layer = (int64_t)mass_rows * cf.n_kv_heads * out_stride;
+  p.kept_stride = kept_stride;
+  p.n_reqs = n_reqs; p.n_layers = n_layers; p.n_kv_heads = cf.n_kv_heads;
+  p.row_chunks = (int32_t)((size_t)cf.head_dim * c->elt / 16);
+  p.max_tokens = (int32_t)longest;
+  p.max_keep = max_keep;
+  hipError_t e = launch_evict_select(p, in_args ? args : nullptr, n_words, c->s_compute);
+  if (e == hipSuccess) e = launch_evict_move(p, in_args ? args : nullptr, n_words, c->s_compute);
+  if (e != hipSuccess) rc = fail_hip(e, "launch of calvo_kv_evict");
   if (!in_args) give_buf(c, buf);
   return rc;
 }
@@ -554,9 +534,9 @@ int calvo_window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_r
     if (dev.status() != hipSuccess) rc = fail_hip(dev.status(), "hipSetDevice");
     else if (capturing(c)) rc = fail(CALVO_EINVAL, "calvo_window_prepare cannot be captured: its tables are read from the host");
     else if ((rc = window_kernels_ready(c)) == CALVO_OK) rc = window_prepare(c, reqs, n_reqs, window, n_first, w);
-    if (rc != CALVO_OK) free_buf(w->buf);
+    if (rc != CALVO_OK) free_buf(c, w->buf);
   } catch (const std::bad_alloc&) {
-    free_buf(w->buf);
+    free_buf(c, w->buf);
     rc = fail(CALVO_ENOMEM, "out of host memory");
   }
   if (rc != CALVO_OK) { delete w; return rc; }
