@@ -301,7 +301,7 @@ typedef struct {
  * prepare for which none is makes one, and may wait for the device there (sizes go up in powers of two).  A plan whose calls were captured must
  * outlive the graph's last replay.  It must precede calvo_destroy of its context.
  * Errors (nothing queued): CALVO_EINVAL for NULL pointers, negative counts, window < 1, slot ids outside the pool, repeated inside a request, or
- * that take new tokens and are in another request's table, more than 2^31 - 65537 tokens in a request, more new tokens than a launch holds, on a stream that is being captured;
+ * that take new tokens and are in another request's table, more than 2^31 - 65537 tokens in a request, some 2^31 blocks in a batch, more new tokens than a launch holds, on a stream that is being captured;
  * CALVO_ENOMEM if a request needs more slots than the pool has or a buffer cannot be had. */
 typedef struct calvo_window calvo_window;
 int calvo_window_prepare(calvo_ctx* ctx, const calvo_window_request* reqs, int n_reqs, int32_t window, int32_t n_first, calvo_window** out);

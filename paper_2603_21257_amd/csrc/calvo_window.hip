@@ -156,6 +156,7 @@ int check_window_requests(const calvo_config& cf, SlotMarks& marks, const calvo_
   if (n_reqs < 0) return fail(CALVO_EINVAL, "n_reqs is negative");
   if (n_reqs > 0 && !reqs) return fail(CALVO_EINVAL, "reqs is NULL");
   *total = 0;
+  int64_t blocks = 0;
   for (int r = 0; r < n_reqs; r++) {
     const calvo_window_request& q = reqs[r];
     if (q.n_cached < 0 || q.n_new < 0) return fail(CALVO_EINVAL, "request %d: negative token count", r);
@@ -166,8 +167,10 @@ int check_window_requests(const calvo_config& cf, SlotMarks& marks, const calvo_
     if (tokens > 0 && !q.block_table) return fail(CALVO_EINVAL, "request %d: block_table is NULL", r);
     if (q.reserved != 0) return fail(CALVO_EINVAL, "request %d: reserved must be 0", r);
     *total += q.n_new;
+    blocks += blocks_of(tokens);
   }
   if (*total * (cf.n_q_heads / cf.n_kv_heads) > INT32_MAX - 4096) return fail(CALVO_EINVAL, "too many new tokens");
+  if (blocks + (int64_t)n_reqs * (kTablePad + 2) > INT32_MAX) return fail(CALVO_EINVAL, "too many tokens in the batch");   // places in its tables are 32 bits wide
   // every table by itself, then the slots that new tokens go to: they are in no other table
   const uint32_t mark = new_marks(cf, marks, (uint32_t)n_reqs + 1), stored = mark + (uint32_t)n_reqs;
   for (int r = 0; r < n_reqs; r++) {
