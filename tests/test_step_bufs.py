@@ -174,3 +174,52 @@ def test_a_larger_plan_behind_many_small_ones():
         assert len(set(held)) == 1, held
     finally:
         cb.calvo_destroy(ctx)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 128])
+def test_steps_ahead_of_the_device(dim):
+    """Decoding steps of requests whose tables outgrow several sizes of buffers, with chunks and evictions in between: the same bits whether the host waits after each
+    call or for none."""
+    import numpy as np
+    import torch
+
+    from paper_2603_21257_amd import binding as cb
+    hq, hkv, steps, blocks = 8, 2, 40, 9000
+    slots = 3 * blocks
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(3)
+    start = torch.randn((1, slots + 8, 2, 16, hkv, dim), dtype=torch.float32, device="cuda:0", generator=gen).to(torch.bfloat16)
+    q = torch.randn((steps, 70, hq, dim), dtype=torch.float32, device="cuda:0", generator=gen).to(torch.bfloat16)
+    k, v = (torch.randn((steps, 70, hkv, dim), dtype=torch.float32, device="cuda:0", generator=gen).to(torch.bfloat16) for _ in range(2))
+    tables = np.random.default_rng(2).permutation(slots).astype(np.int32).reshape(3, blocks)
+
+    def run(wait):
+        pool = start.clone()
+        out, lse = torch.zeros_like(q), torch.zeros(q.shape[:-1], device="cuda:0")
+        stride = 16 * blocks
+        mass = torch.zeros((1, 3, hkv, stride), device="cuda:0")
+        kept = torch.zeros((steps, 1, hkv, 100), dtype=torch.int32, device="cuda:0")
+        torch.cuda.synchronize()
+        ctx = cb.calvo_create(1, hq, hkv, dim, cb.CALVO_BF16, slots + 8, pool)
+        done = (lambda: torch.cuda.synchronize()) if wait else (lambda: None)
+        try:
+            for s in range(steps):
+                # one request has a chunk in every eighth step, the others a token; contexts grow by a quarter a step
+                lens = [(min(16 * blocks - 80, int(40 * 1.25 ** s) + 7 * r), 64 if s % 8 == 5 and r == 1 else 1) for r in range(3)]
+                p = cb.calvo_window_prepare(ctx, [cb.make_window_request(t, c, n, r) for r, (t, (c, n)) in enumerate(zip(tables, lens))], 300, 4)
+                done()
+                cb.calvo_window_attn(p, 0, q[s], k[s], v[s], out[s], lse[s])
+                done()
+                cb.calvo_attn_mass(p, 0, q[s], lse[s], mass, mass, 3, stride)
+                done()
+                cb.calvo_window_destroy(p)
+                if lens[0][0] > 100:
+                    cb.calvo_kv_evict(ctx, [cb.make_evict_request(tables[0], lens[0][0], np.arange(slots, slots + 7), 100, 4, 16)], 0, 1, mass, 3, stride, kept[s], 100)
+                    done()
+        finally:
+            cb.calvo_destroy(ctx)
+        torch.cuda.synchronize()
+        return [x.view(torch.int16) if x.dtype == torch.bfloat16 else x for x in (out, lse, mass, kept, pool)]
+
+    assert all(torch.equal(a, b) for a, b in zip(run(True), run(False)))
