@@ -290,7 +290,8 @@ typedef struct {
                                  the call only.  A slot that takes new tokens is in no other request's table of the batch */
   int32_t n_cached;           /* >= 0 */
   int32_t n_new;              /* >= 0 */
-  int32_t mass_row;           /* row of the request in the arrays of calvo_attn_mass (-1: the plan is not used for it, and plans less) */
+  int32_t mass_row;           /* row of the request in the arrays of calvo_attn_mass (-1 in any request: calvo_attn_mass
+                                 refuses the batch, and prepare leaves its plan out) */
   int32_t reserved;           /* 0 */
 } calvo_window_request;
 
@@ -299,7 +300,8 @@ typedef struct {
  * so that launches and captured graphs of different plans do not meet; those of one plan must not run at the same time.
  * calvo_window_destroy does not wait: the buffer is used again behind the launches that were queued, by plans that it is large enough for.  A
  * prepare for which none is makes one, and may wait for the device there (sizes go up in powers of two).  A plan whose calls were captured must
- * outlive the graph's last replay.  It must precede calvo_destroy of its context.
+ * outlive the graph's last replay.  calvo_window_destroy must precede calvo_destroy of the context.
+ * The host's time grows with the tables, and where no mass_row is -1 with the gathered weights' plan too: 32 requests of 131072 tokens 279 us, 164 without.
  * Errors (nothing queued): CALVO_EINVAL for NULL pointers, negative counts, window < 1, slot ids outside the pool, repeated inside a request, or
  * that take new tokens and are in another request's table, more than 2^31 - 65537 tokens in a request, some 2^31 blocks in a batch, more new tokens than a launch holds, on a stream that is being captured;
  * CALVO_ENOMEM if a request needs more slots than the pool has or a buffer cannot be had. */
@@ -311,7 +313,8 @@ int calvo_window_destroy(calvo_window* w);
  * 2. out[i][h][:] = sum_t softmax_t(scale * <q[i][h], K[t][g]>) V[t][g] over the positions t that the row sees, g = h / (Hq/Hkv);
  * 3. if lse is given, lse[i][h] = ln sum_t exp(scale * <q[i][h], K[t][g]>) over the same positions.
  * q, out: DEVICE [new tokens of the batch][Hq][D], requests one after the other, 16-byte aligned; k_new, v_new: DEVICE [new tokens][Hkv][D];
- * lse: DEVICE fp32 [new tokens][Hq] or NULL.  Element type, accumulation, rounding and scale as calvo_prefill_attn.  K and V of
+ * lse: DEVICE fp32 [new tokens][Hq] or NULL.  Element type, accumulation, rounding and scale as calvo_prefill_attn; one kernel serves the batch, so
+ * the last bits of a request's results may depend on the requests beside it.  K and V of
  * positions that a row does not see never reach its results, whatever they hold; nor does what lies behind a request's last
  * token in its last slot.  Can be captured into a graph (k_new and v_new included): a captured call cannot wait for a load and gets
  * CALVO_ENOTREADY while one is under way.  Errors (nothing queued): CALVO_EINVAL for a bad layer, NULL or misaligned pointers, out, lse or the

@@ -98,7 +98,8 @@ __device__ inline unsigned bf16_rne(float x) {
 __device__ inline float bf16_widen(unsigned b) { return __builtin_bit_cast(float, b << 16); }
 
 // Partial results that other workgroups of the launch read: relaxed atomics of the device's scope go through the caches of an XCD to where all of them
-// meet, and are there when they have been waited for.
+// meet, and are there when they have been waited for.  That is what the hardware does with such accesses, counted by vmcnt; the language's memory model
+// would ask for a release and an acquire around the counter.
 __device__ inline void store_through(float* a, float x, float y) {
   __hip_atomic_store((unsigned long long*)a, __builtin_bit_cast(unsigned long long, (f32x2){x, y}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
