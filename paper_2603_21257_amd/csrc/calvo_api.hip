@@ -441,6 +441,7 @@ void loader_main(calvo_ctx* c, L3Job job) {
   hipError_t e = hipSetDevice(c->device);
   if (e != hipSuccess) hip_fail(e, "hipSetDevice (loader)");
   auto link_free_at = clock::now();          // when the emulated link can start its next chunk
+  auto link_busy_to = link_free_at;          // the end of what l3_busy_s counts so far
   uint64_t k = 0;
   // blocks [j0, j0 + nb) of request q, layer l (nb <= chunk_blocks): through one ring slot
   auto move_chunk = [&](int l, const L3Request& q, int64_t j0, int64_t nb) {
@@ -467,11 +468,17 @@ void loader_main(calvo_ctx* c, L3Job job) {
     const auto start = waited > 50e-6 ? std::max(t1, link_free_at) : link_free_at;
     parallel_copy((unsigned char*)c->l2_ring[slot],
                   q.src + (int64_t)l * q.layer_stride + j0 * (int64_t)c->blk_bytes, bytes, job.n_threads);
+    auto end = clock::now();
+    auto begin = t1;
     if (job.rate > 0.0) {
       link_free_at = start + std::chrono::duration_cast<clock::duration>(std::chrono::duration<double>((double)bytes / job.rate));
       std::this_thread::sleep_until(link_free_at);
+      // the link's own time: it went on while this thread handed the chunk before over, and was free before the thread woke up
+      end = std::max(end, link_free_at);
+      begin = std::max(start, link_busy_to);
     }
-    st.l3_busy_s += std::chrono::duration<double>(clock::now() - t1).count();
+    st.l3_busy_s += std::max(0.0, std::chrono::duration<double>(end - begin).count());
+    link_busy_to = end;
     st.bytes += (int64_t)bytes;
     st.chunks++;
     e = enqueue_staged(c, (const unsigned char*)c->l2_ring[slot], pool_layer, c->d_tab_ing + q.tab_off + j0, nb,
