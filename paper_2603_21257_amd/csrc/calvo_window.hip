@@ -86,7 +86,7 @@ struct StepDev {
   }
 };
 
-// The caller gives the buffer back, also after an error.
+// After an error the caller frees what was made.
 int take_buf(calvo_ctx* c, size_t d_bytes, size_t h_bytes, StepBuf& out) {
   StepDev dev{c};
   return c->step_bufs.take(dev, d_bytes, h_bytes, out);
