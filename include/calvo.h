@@ -21,13 +21,20 @@
  *    from hipHostMalloc (or a framework's pinned allocator).  The library never
  *    frees, reallocates or keeps caller memory beyond what each call states.
  *  - Element type: CALVO_BF16 (2 bytes, upper half of an IEEE fp32) or
- *    CALVO_F32.  The ingest path moves bytes and does not interpret them.
+ *    CALVO_F32; CALVO_E4M3: a pool of 8-bit floats (below), with q, K, V and out in bf16.
+ *    The ingest path moves bytes and does not interpret them.
  *
  * Layouts (B = block_tokens, Hkv = n_kv_heads, D = head_dim; C order)
  *    pool      [n_layers][pool_blocks][2][B][Hkv][D]   2 = K then V
  *    host KV   [n_layers][host blocks][2][B][Hkv][D]   one layer every host_layer_stride bytes
  *    q, out    [total suffix tokens][Hq][D]            requests concatenated, see cu_suffix
  *    k_suffix, v_suffix  [total suffix tokens][Hkv][D]
+ * CALVO_E4M3: a block (in the pool and in host KV) is
+ *    K [Hkv][B][D] bytes, V [Hkv][D][B] bytes, scales fp32 [K, V][Hkv], and room up to a multiple of 128 bytes (calvo_block_bytes)
+ * A byte is an 8-bit float of the OCP format E4M3 (four bits of exponent, three of fraction, largest 448, no infinity, 0x7f and 0xff NaN) and
+ * stands for its value times the scale of its K or V, block and head.  A scale is a power of two, 2^-126 to 2^119: only its exponent is looked at;
+ * one that is not finite makes all its values NaN.  Loading moves such blocks as any others, at half the bytes of bf16; calvo_window_prepare,
+ * calvo_kv_append, calvo_window_attn and the calls without a pool take them, the others refuse with CALVO_EINVAL.
  * The paper names blocks, tiers and the context/query split but no block size,
  * layout or precision; these are this library's definitions.
  *
@@ -66,16 +73,16 @@ extern "C" {
 typedef struct calvo_ctx calvo_ctx; /* opaque: streams, staging buffers, per-layer events, table cache */
 
 enum { CALVO_OK = 0, CALVO_EINVAL = -1, CALVO_ENOMEM = -2, CALVO_EHIP = -3, CALVO_ENOTREADY = -4 };
-enum { CALVO_BF16 = 0, CALVO_F32 = 1 };
+enum { CALVO_BF16 = 0, CALVO_F32 = 1, CALVO_E4M3 = 2 };
 enum { CALVO_EV_QUERY = 0, CALVO_EV_HOST_WAIT = 1, CALVO_EV_STREAM_WAIT = 2 };
 
 typedef struct {
   int32_t n_layers;
   int32_t n_q_heads;     /* multiple of n_kv_heads */
   int32_t n_kv_heads;
-  int32_t head_dim;      /* multiple of 8, at most 256; the bf16 MFMA kernel needs 128 */
+  int32_t head_dim;      /* multiple of 8 (CALVO_E4M3: 16), at most 256; the bf16 MFMA kernel needs 128 */
   int32_t block_tokens;  /* B; must be 16 */
-  int32_t dtype;         /* CALVO_BF16 or CALVO_F32 */
+  int32_t dtype;         /* CALVO_BF16, CALVO_F32 or CALVO_E4M3 */
   int64_t pool_blocks;   /* slots per layer */
   void*   pool;          /* DEVICE, caller-owned, 16-byte aligned; must outlive the context */
   size_t  staging_bytes; /* size of each device staging buffer (a whole number of blocks is used);
@@ -104,6 +111,9 @@ typedef struct {
                                         shared with an earlier request) and are not loaded; usually 0 */
   int32_t        suffix_len;         /* S >= 0 */
 } calvo_request;
+
+/* Bytes of one block in the pool and in host memory, K and V (host code; cfg->pool is not looked at). */
+int calvo_block_bytes(const calvo_config* cfg, int64_t* bytes);
 
 /* Create a context for one pool.  Allocates the staging ring, one event per layer, room for the partial
  * results of cut contexts (68 MB for bf16 pools of head dim 128, 34 MB for others) and
@@ -309,7 +319,8 @@ typedef struct calvo_window calvo_window;
 int calvo_window_prepare(calvo_ctx* ctx, const calvo_window_request* reqs, int n_reqs, int32_t window, int32_t n_first, calvo_window** out);
 int calvo_window_destroy(calvo_window* w);
 
-/* One layer of the batch: 1. if k_new / v_new are given, the new tokens' K and V are written to their slots (NULL: they are there);
+/* One layer of the batch: 1. if k_new / v_new are given, the new tokens' K and V are written to their slots (NULL: they are there; CALVO_E4M3 pools: as
+ * calvo_kv_append without a rope does, and what follows sees the values as they are held);
  * 2. out[i][h][:] = sum_t softmax_t(scale * <q[i][h], K[t][g]>) V[t][g] over the positions t that the row sees, g = h / (Hq/Hkv);
  * 3. if lse is given, lse[i][h] = ln sum_t exp(scale * <q[i][h], K[t][g]>) over the same positions.
  * q, out: DEVICE [new tokens of the batch][Hq][D], requests one after the other, 16-byte aligned; k_new, v_new: DEVICE [new tokens][Hkv][D];
@@ -320,6 +331,31 @@ int calvo_window_destroy(calvo_window* w);
  * CALVO_ENOTREADY while one is under way.  Errors (nothing queued): CALVO_EINVAL for a bad layer, NULL or misaligned pointers, out, lse or the
  * layer's pool overlapping each other or an input. */
 int calvo_window_attn(calvo_window* w, int layer, const void* q, const void* k_new, const void* v_new, void* out, float* lse, float scale);
+
+/* The rotation of Q and K by position.  With a_i = position * inv_freq[i] for i < rot_dim / 2, every pair of a head's first rot_dim elements -
+ * i and i + rot_dim / 2, or 2i and 2i + 1 - goes from (x, y) to (x cos a_i - y sin a_i, y cos a_i + x sin a_i); the others stay as they are. */
+typedef struct {
+  const float*   inv_freq;    /* DEVICE fp32 [rot_dim / 2]: radians from one position to the next */
+  const int32_t* positions;   /* DEVICE int32 [new tokens of the batch], any values; or NULL: token i of a request is at n_cached + i.  (Behind an
+                                 eviction the next token's position is no longer the number of cached ones.) */
+  int32_t rot_dim;            /* even, in [2, head_dim] */
+  int32_t interleaved;        /* 0: pairs (i, i + rot_dim / 2), 1: pairs (2i, 2i + 1) */
+  int64_t reserved;           /* 0 */
+} calvo_rope;
+
+/* One layer of the batch: the new tokens' K (rotated, if rope is given) and V are written to their slots, and q, rotated in the same way, to q_out, where
+ * calvo_window_attn with k_new = v_new = NULL takes it.  k_new, v_new: DEVICE [new tokens of the batch][Hkv][D], rows k_stride and v_stride elements apart;
+ * q: DEVICE [new tokens][Hq][D], rows q_stride apart (a stride of 0: rows that follow each other; q, k_new and v_new may be parts of the rows of one
+ * array); q_out: DEVICE [new tokens][Hq][D].  k_new and v_new may both be NULL (q alone), q and q_out too.  rope == NULL rotates nothing.
+ * Angles are made in 64 bits and sums in fp32; each result is rounded once, to the type of q_out or of the pool.
+ * CALVO_E4M3 pools: q, k_new and v_new are bf16, rotated K is quantised as it comes out of the sum.  A block that takes new tokens is written whole: its
+ * scale (K and V, per head) becomes the smallest power of two s for which every new value is at most 448 s, but not less than that of the tokens it holds
+ * already; where the scale grows these are rounded again to the larger one (exact, but for values below 2^-6 of it); room behind the last token becomes zeros.  A
+ * NaN or an infinity among the new values makes that scale NaN: all values of the block and head read as NaN.
+ * Can be captured, as calvo_window_attn.  Errors (nothing queued): CALVO_EINVAL for a bad layer, misaligned pointers (16 bytes), strides below a row or that
+ * are not whole 16 bytes, a rope outside the limits above, q_out or the layer's pool overlapping each other or an input. */
+int calvo_kv_append(calvo_window* w, int layer, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const void* q, int64_t q_stride,
+                    void* q_out, const calvo_rope* rope);
 
 /* The weight that every token of a request has gathered, per KV head: with R = the request's mass_row,
  *     mass_out[R][g][t] = (t < n_cached ? mass_in[R][g][t] : 0) + sum over the counted rows i that see t and the query heads h of g of

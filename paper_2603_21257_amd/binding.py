@@ -17,14 +17,14 @@ from typing import Optional, Sequence
 import numpy as np
 
 CALVO_OK, CALVO_EINVAL, CALVO_ENOMEM, CALVO_EHIP, CALVO_ENOTREADY = 0, -1, -2, -3, -4
-CALVO_BF16, CALVO_F32 = 0, 1
+CALVO_BF16, CALVO_F32, CALVO_E4M3 = 0, 1, 2
 CALVO_EV_QUERY, CALVO_EV_HOST_WAIT, CALVO_EV_STREAM_WAIT = 0, 1, 2
 
 # CALVO_LIB names another build of the library (A/B timing of two builds); default: the in-tree one
 LIB_PATH = os.environ.get("CALVO_LIB") or os.path.join(os.path.dirname(os.path.abspath(__file__)), "libcalvo.so")
 EXPORTS = ["calvo_create", "calvo_destroy", "calvo_kv_ingest", "calvo_kv_ingest_chunked", "calvo_chunk_count",
            "calvo_chunk_event", "calvo_kv_ingest_l3", "calvo_l3_wait", "calvo_layer_event", "calvo_prefill_attn", "calvo_prefill_attn_noalloc", "calvo_batch_prepare", "calvo_batch_destroy", "calvo_prefill_attn_batch",
-           "calvo_window_prepare", "calvo_window_destroy", "calvo_window_attn", "calvo_attn_mass", "calvo_kv_evict",
+           "calvo_window_prepare", "calvo_window_destroy", "calvo_window_attn", "calvo_kv_append", "calvo_block_bytes", "calvo_attn_mass", "calvo_kv_evict",
            "calvo_window_plan", "calvo_evict_check", "calvo_attn_kernel_ms", "calvo_mfma_peak", "calvo_attn_kernel_info", "calvo_attn_tile_rows", "calvo_attn_plan", "calvo_attn_plan_items", "calvo_ingest_plan", "calvo_cost_fit", "calvo_cost_estimate",
            "calvo_sched_pick", "calvo_sched_simulate", "calvo_pool_create", "calvo_pool_destroy", "calvo_pool_reserve",
            "calvo_pool_retain", "calvo_pool_release", "calvo_pool_counts", "calvo_pool_admit", "calvo_pool_retry",
@@ -49,6 +49,10 @@ class calvo_request(C.Structure):
 class calvo_window_request(C.Structure):
     _fields_ = [("block_table", C.POINTER(C.c_int32)), ("n_cached", C.c_int32), ("n_new", C.c_int32), ("mass_row", C.c_int32),
                 ("reserved", C.c_int32)]
+
+
+class calvo_rope(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("positions", C.c_void_p), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("reserved", C.c_int64)]
 
 
 class calvo_evict_request(C.Structure):
@@ -138,6 +142,9 @@ def lib() -> C.CDLL:
         L.calvo_window_prepare.argtypes = [C.c_void_p, C.POINTER(calvo_window_request), C.c_int, C.c_int32, C.c_int32, C.POINTER(C.c_void_p)]
         L.calvo_window_destroy.argtypes = [C.c_void_p]
         L.calvo_window_attn.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float]
+        L.calvo_kv_append.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                      C.POINTER(calvo_rope)]
+        L.calvo_block_bytes.argtypes = [C.POINTER(calvo_config), C.POINTER(C.c_int64)]
         L.calvo_attn_mass.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int32,
                                       C.c_float]
         L.calvo_kv_evict.argtypes = [C.c_void_p, C.POINTER(calvo_evict_request), C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int32, C.c_int64,
@@ -373,6 +380,26 @@ def calvo_window_destroy(window: int) -> None:
 
 def calvo_window_attn(window: int, layer: int, q, k_new, v_new, out, lse=None, scale: float = 0.0) -> None:
     _check(lib().calvo_window_attn(window, layer, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(lse), float(scale)))
+
+
+def make_rope(inv_freq, rot_dim: int, interleaved: bool = False, positions=None) -> calvo_rope:
+    """The rotation of calvo_kv_append; inv_freq and positions in device memory.  The returned struct keeps them alive."""
+    r = calvo_rope(_ptr(inv_freq), _ptr(positions), int(rot_dim), int(interleaved), 0)
+    r._keep = (inv_freq, positions)
+    return r
+
+
+def calvo_kv_append(window: int, layer: int, k_new, v_new, q=None, q_out=None, rope: Optional[calvo_rope] = None, k_stride: int = 0,
+                    v_stride: int = 0, q_stride: int = 0) -> None:
+    """Strides in elements from one token's row to the next; 0: rows that follow each other."""
+    _check(lib().calvo_kv_append(window, layer, _ptr(k_new), int(k_stride), _ptr(v_new), int(v_stride), _ptr(q), int(q_stride), _ptr(q_out), rope))
+
+
+def calvo_block_bytes(n_kv_heads: int, head_dim: int, dtype: int) -> int:
+    """Bytes of one block of 16 tokens, K and V, in the pool and in host memory."""
+    out = C.c_int64()
+    _check(lib().calvo_block_bytes(C.byref(_shape_config(n_kv_heads, n_kv_heads, head_dim, dtype, 1)), C.byref(out)))
+    return out.value
 
 
 def calvo_attn_mass(window: int, layer: int, q, lse, mass_in, mass_out, mass_rows: int, mass_stride: int, last_rows: int = 0,

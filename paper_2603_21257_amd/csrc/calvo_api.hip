@@ -18,6 +18,7 @@
 
 #include "calvo_ctx.h"
 #include "ingest_plan.h"
+#include "kv_e4m3.h"
 #include "window_plan.h"
 
 using namespace calvo;
@@ -139,6 +140,16 @@ void destroy_partial(calvo_ctx* c) {
 namespace calvo {
 namespace host {
 
+size_t block_bytes(const calvo_config& cfg) {
+  if (cfg.dtype == CALVO_E4M3) return (size_t)e4m3_block(cfg.n_kv_heads, cfg.head_dim).bytes;
+  return (size_t)2 * kBlockTokens * cfg.n_kv_heads * cfg.head_dim * (cfg.dtype == CALVO_BF16 ? 2 : 4);
+}
+
+int not_for_e4m3(const calvo_config& cfg, const char* what) {
+  if (cfg.dtype != CALVO_E4M3) return CALVO_OK;
+  return fail(CALVO_EINVAL, "%s does not take an 8-bit pool (CALVO_E4M3)", what);
+}
+
 int validate_config(const calvo_config* cfg) {
   if (!cfg) return fail(CALVO_EINVAL, "config is NULL");
   if (cfg->n_layers <= 0) return fail(CALVO_EINVAL, "n_layers must be positive");
@@ -148,15 +159,17 @@ int validate_config(const calvo_config* cfg) {
   if (cfg->head_dim <= 0 || cfg->head_dim > 256 || cfg->head_dim % 8 != 0)
     return fail(CALVO_EINVAL, "head_dim must be a multiple of 8 in [8, 256]");
   if (cfg->block_tokens != kBlockTokens) return fail(CALVO_EINVAL, "block_tokens must be 16");
-  if (cfg->dtype != CALVO_BF16 && cfg->dtype != CALVO_F32) return fail(CALVO_EINVAL, "unknown dtype");
+  if (cfg->dtype != CALVO_BF16 && cfg->dtype != CALVO_F32 && cfg->dtype != CALVO_E4M3) return fail(CALVO_EINVAL, "unknown dtype");
+  if (cfg->dtype == CALVO_E4M3 && cfg->head_dim % 16 != 0) return fail(CALVO_EINVAL, "head_dim must be a multiple of 16 in an 8-bit pool");
   if (cfg->pool_blocks <= 0 || cfg->pool_blocks > INT32_MAX) return fail(CALVO_EINVAL, "pool_blocks out of range");
   if (!cfg->pool) return fail(CALVO_EINVAL, "pool is NULL");
   if (((uintptr_t)cfg->pool & 15) != 0) return fail(CALVO_EINVAL, "pool must be 16-byte aligned");
   if (cfg->n_staging != 0 && (cfg->n_staging < 2 || cfg->n_staging > 8))
     return fail(CALVO_EINVAL, "n_staging must be 0 or in [2, 8]");
   if (cfg->n_copy_streams < 0 || cfg->n_copy_streams > 1) return fail(CALVO_EINVAL, "n_copy_streams must be 0 or 1");
-  const size_t elt = cfg->dtype == CALVO_BF16 ? 2 : 4;
-  const size_t blk = (size_t)2 * kBlockTokens * cfg->n_kv_heads * cfg->head_dim * elt;
+  if (cfg->dtype == CALVO_E4M3 && cfg->n_kv_heads > (1 << 30) / (2 * kBlockTokens * cfg->head_dim))
+    return fail(CALVO_EINVAL, "a block of an 8-bit pool must be smaller than 1 GiB");
+  const size_t blk = block_bytes(*cfg);
   if (cfg->staging_bytes != 0 && cfg->staging_bytes < blk)
     return fail(CALVO_EINVAL, "staging_bytes (%zu) is smaller than one block (%zu)", cfg->staging_bytes, blk);
   return CALVO_OK;
@@ -349,6 +362,11 @@ int queue_behind_layer(calvo_ctx* c, int layer) {
 int window_kernels_ready(calvo_ctx* c) {
   if (c->window_kernels) return CALVO_OK;
   const bool f32 = c->cfg.dtype == CALVO_F32;
+  if (c->cfg.dtype == CALVO_E4M3) {
+    for (const int rows : {16, 32}) HIP_TRY(attn_e4m3_prepare(c->cfg.head_dim, rows));
+    c->window_kernels = true;
+    return CALVO_OK;
+  }
   HIP_TRY(attn_window_prepare(c->cfg.dtype, c->cfg.head_dim, attn_rows_shape(f32, c->cfg.head_dim, false).tile_rows));
   if (attn_rows_has_large(f32, c->cfg.head_dim))
     HIP_TRY(attn_window_prepare(c->cfg.dtype, c->cfg.head_dim, attn_rows_shape(f32, c->cfg.head_dim, true).tile_rows));
@@ -557,8 +575,8 @@ int calvo_create(const calvo_config* cfg, calvo_ctx** out) {
     if (hipDeviceGetAttribute(&khz, hipDeviceAttributeWallClockRate, dev) == hipSuccess && khz > 0) c->clock_khz = khz;
     else (void)hipGetLastError();
   }
-  c->elt = cfg->dtype == CALVO_BF16 ? 2 : 4;
-  c->blk_bytes = (size_t)2 * kBlockTokens * cfg->n_kv_heads * cfg->head_dim * c->elt;
+  c->elt = cfg->dtype == CALVO_F32 ? 4 : 2;
+  c->blk_bytes = block_bytes(*cfg);
   c->layer_bytes = (int64_t)cfg->pool_blocks * (int64_t)c->blk_bytes;
   c->n_staging = cfg->staging_bytes ? (cfg->n_staging ? cfg->n_staging : 2) : 0;
   c->n_copy = cfg->n_copy_streams ? cfg->n_copy_streams : 1;
@@ -634,7 +652,7 @@ int calvo_create(const calvo_config* cfg, calvo_ctx** out) {
     if (e == hipSuccess) e = attn_duo_prepare();
     if (e != hipSuccess) { const int prc = fail_hip(e, "hipFuncSetAttribute(dynamic LDS)"); destroy_partial(c); return prc; }
   }
-  if (!(cfg->dtype == CALVO_BF16 && cfg->head_dim == 128)) {
+  if (cfg->dtype != CALVO_E4M3 && !(cfg->dtype == CALVO_BF16 && cfg->head_dim == 128)) {
     const bool f32 = cfg->dtype == CALVO_F32;
     hipError_t e = attn_rows_prepare(cfg->dtype, cfg->head_dim, attn_rows_shape(f32, cfg->head_dim, false).tile_rows);
     if (e == hipSuccess && attn_rows_has_large(f32, cfg->head_dim))
@@ -1521,6 +1539,10 @@ void free_prepared(calvo_ctx* c, PreparedPlan& pp) {
 int calvo::host::prefill_attn_impl(calvo_ctx* c, int layer, const void* q, const void* k_suffix, const void* v_suffix, void* out,
                                    const calvo_request* reqs, int n_reqs, const int32_t* cu_suffix, float scale, bool use_static,
                                    hipEvent_t ready) {
+  if (c) {
+    const int no = not_for_e4m3(c->cfg, "calvo_prefill_attn");
+    if (no != CALVO_OK) return no;
+  }
   if (!c) return fail(CALVO_EINVAL, "ctx is NULL");
   if (layer < 0 || layer >= c->cfg.n_layers) return fail(CALVO_EINVAL, "layer %d outside [0, %d)", layer, c->cfg.n_layers);
   KeptBatch* kept = (KeptBatch*)c->kept.get();
@@ -1683,7 +1705,8 @@ int calvo_batch_prepare(calvo_ctx* c, const calvo_request* reqs, int n_reqs, con
   *out = nullptr;
   if (!c) return fail(CALVO_EINVAL, "ctx is NULL");
   int total = 0;
-  int rc = check_batch_args(c, reqs, n_reqs, cu_suffix, &total);
+  int rc = not_for_e4m3(c->cfg, "calvo_batch_prepare");
+  if (rc == CALVO_OK) rc = check_batch_args(c, reqs, n_reqs, cu_suffix, &total);
   if (rc != CALVO_OK) return rc;
   calvo_batch* b = new (std::nothrow) calvo_batch();
   if (!b) return fail(CALVO_ENOMEM, "out of host memory");
@@ -1715,6 +1738,16 @@ int calvo_batch_destroy(calvo_batch* b) {
   batch_free_completed(b);
   if (e != hipSuccess) return fail_hip(e, "synchronize at calvo_batch_destroy");
   return CALVO_OK;
+}
+
+int calvo_block_bytes(const calvo_config* cfg, int64_t* bytes) {
+  if (!cfg || !bytes) return fail(CALVO_EINVAL, "NULL argument");
+  calvo_config cf = *cfg;
+  cf.pool = (void*)16;                         // not looked at
+  cf.staging_bytes = 0;
+  const int rc = validate_config(&cf);
+  if (rc == CALVO_OK) *bytes = (int64_t)block_bytes(cf);
+  return rc;
 }
 
 int calvo_prefill_attn_batch(calvo_ctx* c, calvo_batch* b, int layer, const void* q, const void* k_suffix, const void* v_suffix,

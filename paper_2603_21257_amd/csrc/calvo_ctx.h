@@ -172,6 +172,12 @@ int queue_behind_layer(calvo_ctx* c, int layer);
 // shape, element type, pool and staging sizes of a configuration
 int validate_config(const calvo_config* cfg);
 
+// bytes of a block, K and V (and scales)
+size_t block_bytes(const calvo_config& cfg);
+
+// CALVO_EINVAL for a pool of 8-bit floats
+int not_for_e4m3(const calvo_config& cfg, const char* what);
+
 // Raises the LDS limits of the window kernels for the context's shape, once
 int window_kernels_ready(calvo_ctx* c);
 

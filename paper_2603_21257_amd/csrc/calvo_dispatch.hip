@@ -460,6 +460,10 @@ int calvo_dispatch_create(calvo_ctx* c, const calvo_dispatch_config* cfg, calvo_
   *out = nullptr;
   if (!cfg) return fail(CALVO_EINVAL, "config is NULL");
   if (cfg->policy < CALVO_POLICY_FIFO || cfg->policy > CALVO_POLICY_EDF) return fail(CALVO_EINVAL, "unknown policy %d", cfg->policy);
+  if (c) {
+    const int no = not_for_e4m3(c->cfg, "the dispatcher");
+    if (no != CALVO_OK) return no;
+  }
   if (c && c->n_staging == 0) return fail(CALVO_EINVAL, "the dispatcher needs a context with staging buffers");
   const calvo_l3_config& l3 = cfg->l3;
   if (cfg->three_stage) {

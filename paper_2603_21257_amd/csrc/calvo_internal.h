@@ -162,6 +162,31 @@ hipError_t launch_attn_window(const WinParams& p, int dtype, int tile_rows, int 
 hipError_t attn_window_pipe_prepare();
 hipError_t launch_attn_window_pipe(const WinParams& p, int variant, int n_items, const int32_t* split_tiles, int n_split_tiles, hipStream_t stream);
 
+// the same over pools of CALVO_E4M3 (attn_e4m3.hip): work items count 64-key steps
+hipError_t attn_e4m3_prepare(int head_dim, int tile_rows);
+hipError_t launch_attn_e4m3(const WinParams& p, int tile_rows, int n_items, const int32_t* split_tiles, int n_split_tiles, hipStream_t stream);
+
+// ---- appending new tokens with the rotation by position (kv_append.hip)
+struct RopeParams {
+  const float* inv_freq;     // or NULL: no rotation
+  const int32_t* positions;  // or NULL: behind the cached tokens
+  int32_t rot, half;         // rotated elements of a head; half of them
+  int32_t interleaved;
+};
+struct KvAppendParams {
+  const void *q, *k, *v;     // q, or k and v, may be NULL
+  void* q_out;
+  int64_t q_row, k_row, v_row;   // bytes from one token's row to the next
+  unsigned char* pool_layer;
+  const ReqDesc* reqs;
+  const int32_t* touched;    // CALVO_E4M3: blocks that the requests in front of one write, [n_reqs + 1]
+  const int32_t* tables;
+  int32_t n_reqs, total_tokens, n_touched;
+  int32_t n_q_heads, n_kv_heads, head_dim;
+  RopeParams rope;
+};
+hipError_t launch_kv_append(const KvAppendParams& p, int dtype, int n_cus, hipStream_t stream);
+
 // A work item of the gathered weights: key tile `tile` of a request (attn_mass_tile_keys keys) and those of the new tokens [begin, end) whose rows
 // see it.  part: where the sums go if the tile has several items, else -1
 struct MassItem {

@@ -24,7 +24,8 @@ struct calvo_window {
   MassPlan mass;
   StepBuf buf;
   // 32-bit words from the beginning of buf.d
-  size_t items_at = 0, split_at = 0, arrived_at = 0, mass_at = 0, add_at = 0, append_at = 0, tables_at = 0, offs_at = 0;
+  size_t items_at = 0, split_at = 0, arrived_at = 0, mass_at = 0, add_at = 0, append_at = 0, touched_at = 0, tables_at = 0, offs_at = 0;
+  int n_touched = 0;                    // blocks that new tokens go to
   size_t part_o_at = 0, part_ml_at = 0, part_mass_at = 0; // floats, behind them
 };
 
@@ -255,10 +256,11 @@ int window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, i
   w->mass_rows_differ = std::adjacent_find(rows_used.begin(), rows_used.end()) == rows_used.end() && (rows_used.empty() || rows_used.front() >= 0);
   w->max_mass_row = rows_used.empty() ? -1 : rows_used.back();
 
-  plan_window({cf.dtype == CALVO_F32, cf.head_dim, cf.n_q_heads, cf.n_kv_heads, c->n_cus, c->force_splits, c->force_rows_tile, forced_variant()}, lens,
+  plan_window({cf.dtype == CALVO_F32, cf.head_dim, cf.n_q_heads, cf.n_kv_heads, c->n_cus, c->force_splits, c->force_rows_tile, forced_variant(), cf.dtype == CALVO_E4M3}, lens,
               window, n_first, w->plan);
+  const bool e4m3 = cf.dtype == CALVO_E4M3;
   const int tile_keys = attn_mass_tile_keys(cf.dtype, cf.head_dim);
-  if (w->mass_rows_differ)                // else calvo_attn_mass refuses the plan (32 requests of 300 to 33000 tokens: 28 us with it, 21 without)
+  if (w->mass_rows_differ && !e4m3)                // else calvo_attn_mass refuses the plan (32 requests of 300 to 33000 tokens: 28 us with it, 21 without)
     plan_mass(cf.n_q_heads / cf.n_kv_heads, cf.n_kv_heads, c->n_cus, tile_keys, lens, window, n_first, w->mass);
   const size_t n_mass = w->mass.items.size();
   if ((int64_t)n_mass * cf.n_kv_heads * std::max(256, tile_keys) > kMostThreads) return fail(CALVO_EINVAL, "too many tokens in the batch");
@@ -277,7 +279,8 @@ int window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, i
   w->mass_at = pad4(w->arrived_at + n_arrived);
   w->add_at = w->mass_at + n_mass * kMass;
   w->append_at = w->add_at + w->mass.adds.size() * kAdd;
-  w->tables_at = w->append_at + (size_t)n_reqs * kApp;
+  w->touched_at = w->append_at + (size_t)n_reqs * kApp;
+  w->tables_at = w->touched_at + (e4m3 ? (size_t)n_reqs + 1 : 0);
   w->offs_at = pad4(w->tables_at + (size_t)table_words);
   auto offs_of = [](int64_t n_tab) { return n_tab + kTablePad + (n_tab & 1); };
   size_t n_offs = 0;
@@ -311,9 +314,12 @@ int window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, i
     h[w->tables_at + at + n_tab] = n_tab ? reqs[r].block_table[n_tab - 1] : 0;
     const ReqDesc a = {(int32_t)at, reqs[r].n_cached, reqs[r].n_new, q};
     memcpy(h + w->append_at + (size_t)r * kApp, &a, sizeof a);
+    if (e4m3) h[w->touched_at + (size_t)r] = w->n_touched;
+    if (reqs[r].n_new) w->n_touched += (int)((int64_t)n_tab - reqs[r].n_cached / kBlockTokens);
     at += n_tab + 1;
     q += reqs[r].n_new;
   }
+  if (e4m3) h[w->touched_at + (size_t)n_reqs] = w->n_touched;
   for (size_t i = 0; i < n_items; i++) {
     const WindowPiece& x = w->plan.items[i];
     const WinItem d = {x.tile, x.sub_begin, x.sub_end, x.n_splits, x.first_item, table_off[x.req], reqs[x.req].n_cached, reqs[x.req].n_new,
@@ -338,6 +344,69 @@ int window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, i
 int check_layer(const calvo_ctx* c, int layer) {
   if (layer < 0 || layer >= c->cfg.n_layers) return fail(CALVO_EINVAL, "layer %d outside [0, %d)", layer, c->cfg.n_layers);
   return CALVO_OK;
+}
+
+// The append's launch: q, k, v, their rows and the rotation are in p
+int queue_append(calvo_window* w, KvAppendParams& p, unsigned char* pool_layer) {
+  calvo_ctx* c = w->c;
+  const calvo_config& cf = c->cfg;
+  const int32_t* d = w->buf.d;
+  p.pool_layer = pool_layer;
+  p.reqs = (const ReqDesc*)(d + w->append_at); p.touched = d + w->touched_at; p.tables = d + w->tables_at;
+  p.n_reqs = w->n_reqs; p.total_tokens = w->total; p.n_touched = w->n_touched;
+  p.n_q_heads = cf.n_q_heads; p.n_kv_heads = cf.n_kv_heads; p.head_dim = cf.head_dim;
+  HIP_TRY(launch_kv_append(p, cf.dtype, c->n_cus, c->s_compute));
+  return CALVO_OK;
+}
+
+int kv_append(calvo_window* w, int layer, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const void* q, int64_t q_stride,
+              void* q_out, const calvo_rope* rope) {
+  calvo_ctx* c = w->c;
+  const calvo_config& cf = c->cfg;
+  int rc = check_layer(c, layer);
+  if (rc != CALVO_OK) return rc;
+  unsigned char* pool_layer = (unsigned char*)cf.pool + (int64_t)layer * c->layer_bytes;
+  KvAppendParams p{};
+  if (rope) {
+    if (rope->reserved != 0) return fail(CALVO_EINVAL, "rope: reserved must be 0");
+    if (rope->rot_dim < 2 || rope->rot_dim > cf.head_dim || rope->rot_dim % 2) return fail(CALVO_EINVAL, "rope: rot_dim must be even and in [2, head_dim]");
+    if (rope->interleaved != 0 && rope->interleaved != 1) return fail(CALVO_EINVAL, "rope: interleaved must be 0 or 1");
+    if (w->total > 0 && !rope->inv_freq) return fail(CALVO_EINVAL, "rope: inv_freq is NULL");
+    if ((((uintptr_t)rope->inv_freq | (uintptr_t)rope->positions) & 3) != 0) return fail(CALVO_EINVAL, "rope: inv_freq and positions must be 4-byte aligned");
+    p.rope = {rope->inv_freq, rope->positions, rope->rot_dim, rope->rot_dim / 2, rope->interleaved};
+  }
+  if ((k_new == nullptr) != (v_new == nullptr)) return fail(CALVO_EINVAL, "k_new and v_new must both be given or both be NULL");
+  if ((q == nullptr) != (q_out == nullptr)) return fail(CALVO_EINVAL, "q and q_out must both be given or both be NULL");
+  if ((((uintptr_t)q | (uintptr_t)q_out | (uintptr_t)k_new | (uintptr_t)v_new) & 15) != 0)
+    return fail(CALVO_EINVAL, "q, q_out, k_new and v_new must be 16-byte aligned");
+  const int64_t kv_row = (int64_t)cf.n_kv_heads * cf.head_dim, q_row = (int64_t)cf.n_q_heads * cf.head_dim, unit = 16 / (int64_t)c->elt;
+  struct { const void* at; int64_t given, row; int64_t* bytes; const char* name; } in[] = {
+      {k_new, k_stride, kv_row, &p.k_row, "k_new"}, {v_new, v_stride, kv_row, &p.v_row, "v_new"}, {q, q_stride, q_row, &p.q_row, "q"}};
+  for (const auto& x : in) {
+    if (!x.at) continue;
+    const int64_t s = x.given ? x.given : x.row;
+    if (s < x.row || s % unit != 0 || s > ((int64_t)1 << 40))
+      return fail(CALVO_EINVAL, "the stride of %s must be 0 or a multiple of %d from %lld on", x.name, (int)unit, (long long)x.row);
+    *x.bytes = s * (int64_t)c->elt;
+  }
+  p.q = q; p.k = k_new; p.v = v_new; p.q_out = q_out;
+  if (w->total > 0) {
+    auto extent = [&](const void* at, int64_t row_bytes, int64_t row, const char* name) {
+      return Range{(uintptr_t)at, (size_t)((w->total - 1) * row_bytes + row * (int64_t)c->elt), name};
+    };
+    const Range to[] = {{(uintptr_t)q_out, (size_t)(w->total * q_row) * c->elt, "q_out"}, {(uintptr_t)pool_layer, (size_t)c->layer_bytes, "the pool"}};
+    const Range from[] = {extent(k_new, p.k_row, kv_row, "k_new"), extent(v_new, p.v_row, kv_row, "v_new"), extent(q, p.q_row, q_row, "q"),
+                          {(uintptr_t)p.rope.inv_freq, (size_t)p.rope.half * 4, "rope: inv_freq"},
+                          {(uintptr_t)p.rope.positions, (size_t)w->total * 4, "rope: positions"}};
+    if ((rc = apart(to[0], to[1])) != CALVO_OK) return rc;
+    for (const Range& a : to)
+      for (const Range& b : from)
+        if ((rc = apart(a, b)) != CALVO_OK) return rc;
+    if (((int64_t)w->n_touched * ((cf.n_kv_heads + 3) / 4) + w->total) * 256 > kMostThreads) return fail(CALVO_EINVAL, "too many new tokens");
+  }
+  ON_DEVICE(c);
+  if ((rc = queue_behind_layer(c, layer)) != CALVO_OK) return rc;
+  return w->total > 0 ? queue_append(w, p, pool_layer) : CALVO_OK;
 }
 
 int window_attn(calvo_window* w, int layer, const void* q, const void* k_new, const void* v_new, void* out, float* lse, float scale) {
@@ -370,8 +439,15 @@ int window_attn(calvo_window* w, int layer, const void* q, const void* k_new, co
   const int32_t* d = w->buf.d;
   // The attention launch stores the new rows itself where every request is one tile of packed rows (decoding) and a head's row is whole cache
   // lines: one launch less.
-  const bool along = k_new && w->plan.single_tiles && (size_t)cf.head_dim * c->elt % 128 == 0;
-  if (k_new && !along) {
+  const bool e4m3 = cf.dtype == CALVO_E4M3;
+  if (k_new && e4m3) {
+    KvAppendParams app{};
+    app.k = k_new; app.v = v_new;
+    app.k_row = app.v_row = (int64_t)cf.n_kv_heads * cf.head_dim * (int64_t)c->elt;
+    if ((rc = queue_append(w, app, pool_layer)) != CALVO_OK) return rc;
+  }
+  const bool along = !e4m3 && k_new && w->plan.single_tiles && (size_t)cf.head_dim * c->elt % 128 == 0;
+  if (k_new && !along && !e4m3) {
     AppendParams app{};
     app.k_suffix = k_new; app.v_suffix = v_new; app.pool_layer = pool_layer;
     app.reqs = (const ReqDesc*)(d + w->append_at); app.tables = d + w->tables_at;
@@ -392,7 +468,8 @@ int window_attn(calvo_window* w, int layer, const void* q, const void* k_new, co
   const int n_items = (int)w->plan.items.size(), n_cut = (int)w->plan.split_tiles.size();
   if (w->plan.variant == kWindowRows) {
     if (w->plan.one_launch) p.arrived = w->buf.d + w->arrived_at;
-    HIP_TRY(launch_attn_window(p, cf.dtype, w->plan.tile_rows, n_items, d + w->split_at, p.arrived ? 0 : n_cut, c->s_compute));
+    if (e4m3) HIP_TRY(launch_attn_e4m3(p, w->plan.tile_rows, n_items, d + w->split_at, p.arrived ? 0 : n_cut, c->s_compute));
+    else HIP_TRY(launch_attn_window(p, cf.dtype, w->plan.tile_rows, n_items, d + w->split_at, p.arrived ? 0 : n_cut, c->s_compute));
   } else {
     p.heads_per_wg = w->plan.heads_per_wg;
     p.row_blocks_per_wg = attn_mfma_row_blocks(w->plan.variant);
@@ -407,6 +484,7 @@ int attn_mass(calvo_window* w, int layer, const void* q, const float* lse, const
   const calvo_config& cf = c->cfg;
   int rc = check_layer(c, layer);
   if (rc != CALVO_OK) return rc;
+  if ((rc = not_for_e4m3(cf, "calvo_attn_mass")) != CALVO_OK) return rc;
   if (cf.n_q_heads / cf.n_kv_heads > 4096) return fail(CALVO_EINVAL, "more than 4096 query heads to a KV head");
   if (mass_rows < 0 || last_rows < 0) return fail(CALVO_EINVAL, "mass_rows and last_rows must not be negative");
   if (w->longest > 0) {
@@ -447,10 +525,11 @@ int kv_evict(calvo_ctx* c, const calvo_evict_request* reqs, int n_reqs, int laye
   const calvo_config& cf = c->cfg;
   if (layer_begin < 0 || layer_end > cf.n_layers || layer_begin > layer_end)
     return fail(CALVO_EINVAL, "layers [%d, %d) outside [0, %d)", layer_begin, layer_end, cf.n_layers);
+  int rc = not_for_e4m3(cf, "calvo_kv_evict");
+  if (rc != CALVO_OK) return rc;
   const int n_layers = layer_end - layer_begin;
   if (n_layers > 65535) return fail(CALVO_EINVAL, "more than 65535 layers");
-  int rc = check_evict_requests(cf, c->marks, reqs, n_reqs, mass_rows);
-  if (rc != CALVO_OK) return rc;
+  if ((rc = check_evict_requests(cf, c->marks, reqs, n_reqs, mass_rows)) != CALVO_OK) return rc;
   int64_t table_words = 0, longest = 0;
   int32_t max_keep = 0;
   for (int r = 0; r < n_reqs; r++) {
@@ -571,10 +650,10 @@ int calvo_window_plan(const calvo_config* cfg, int32_t n_cus, const calvo_window
     std::vector<WindowLens> lens((size_t)n_reqs);
     for (int r = 0; r < n_reqs; r++) lens[r] = {reqs[r].n_cached, reqs[r].n_new};
     WindowPlan plan;
-    plan_window({cf.dtype == CALVO_F32, cf.head_dim, cf.n_q_heads, cf.n_kv_heads, n_cus, 0, 0, forced_variant()}, lens, window, n_first, plan);
+    plan_window({cf.dtype == CALVO_F32, cf.head_dim, cf.n_q_heads, cf.n_kv_heads, n_cus, 0, 0, forced_variant(), cf.dtype == CALVO_E4M3}, lens, window, n_first, plan);
     if (kernel) *kernel = plan.variant;
     int32_t n = 0;
-    const int group = cf.n_q_heads / cf.n_kv_heads;
+    const int group = cf.n_q_heads / cf.n_kv_heads, unit = cf.dtype == CALVO_E4M3 && plan.variant == kWindowRows ? kE4m3Keys / 32 : 1;
     for (const WindowPiece& x : plan.items) {
       const int64_t rows = (int64_t)lens[(size_t)x.req].n_new * group, tr = plan.variant == kWindowRows ? plan.tile_rows : (int64_t)plan.tile_tokens * group;
       // runs of the item's part of the list: where each begins in the list, how many, where in the context
@@ -591,7 +670,7 @@ int calvo_window_plan(const calvo_config* cfg, int32_t n_cus, const calvo_window
         if (n < capacity) {
           int32_t* o = entries + 7 * (int64_t)n;
           o[0] = x.req; o[1] = (int32_t)(x.tile * tr); o[2] = (int32_t)std::min((x.tile + 1) * tr, rows);
-          o[3] = b - runs[i][0] + runs[i][2]; o[4] = e - runs[i][0] + runs[i][2];
+          o[3] = unit * (b - runs[i][0] + runs[i][2]); o[4] = unit * (e - runs[i][0] + runs[i][2]);
           o[5] = listed && i < 2; o[6] = x.n_splits;
         }
         n++;
@@ -608,7 +687,8 @@ int calvo_evict_check(const calvo_config* cfg, const calvo_evict_request* reqs, 
   if (!cfg) return fail(CALVO_EINVAL, "config is NULL");
   calvo_config cf = *cfg;
   cf.pool = (void*)16;
-  const int rc = validate_config(&cf);
+  int rc = validate_config(&cf);
+  if (rc == CALVO_OK) rc = not_for_e4m3(cf, "calvo_kv_evict");
   if (rc != CALVO_OK) return rc;
   try {
     SlotMarks marks;
@@ -621,6 +701,12 @@ int calvo_evict_check(const calvo_config* cfg, const calvo_evict_request* reqs, 
 int calvo_window_attn(calvo_window* w, int layer, const void* q, const void* k_new, const void* v_new, void* out, float* lse, float scale) {
   if (!w) return fail(CALVO_EINVAL, "window is NULL");
   return window_attn(w, layer, q, k_new, v_new, out, lse, scale);
+}
+
+int calvo_kv_append(calvo_window* w, int layer, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const void* q, int64_t q_stride,
+                    void* q_out, const calvo_rope* rope) {
+  if (!w) return fail(CALVO_EINVAL, "window is NULL");
+  return kv_append(w, layer, k_new, k_stride, v_new, v_stride, q, q_stride, q_out, rope);
 }
 
 int calvo_attn_mass(calvo_window* w, int layer, const void* q, const float* lse, const float* mass_in, float* mass_out, int32_t mass_rows,

@@ -6,11 +6,11 @@
 
 namespace calvo {
 
-WindowKeys window_keys(int64_t pos_min, int64_t pos_max, int32_t window, int32_t n_first) {
+WindowKeys window_keys(int64_t pos_min, int64_t pos_max, int32_t window, int32_t n_first, int unit) {
   const int64_t lo = std::max<int64_t>(0, pos_min + 1 - window);      // earliest key of the earliest row's window
-  const int32_t lo_sub = (int32_t)(lo / 32), end = (int32_t)(pos_max / 32 + 1);
+  const int32_t lo_sub = (int32_t)(lo / unit), end = (int32_t)(pos_max / unit + 1);
   WindowKeys k;
-  k.first_subs = (int32_t)std::min<int64_t>(((int64_t)n_first + 31) / 32, lo_sub);
+  k.first_subs = (int32_t)std::min<int64_t>(((int64_t)n_first + unit - 1) / unit, lo_sub);
   k.gap = lo_sub - k.first_subs;
   k.n = k.first_subs + end - lo_sub;
   return k;
@@ -46,6 +46,7 @@ constexpr int64_t kMostSlots = 2048;
 
 struct Candidate {
   int variant = kWindowRows;
+  int unit = 32;                         // packed rows: keys of a sub-tile
   RowsShape shape{};                     // packed rows
   int tile_tokens = 0;                   // pipelined
   PlanParams params{};
@@ -57,7 +58,7 @@ struct Candidate {
 WindowKeys tile_keys(const Candidate& c, const WindowLens& l, int64_t tile, int group, int32_t window, int32_t n_first) {
   if (c.variant == kWindowRows) {
     const int64_t rows = (int64_t)l.n_new * group, tr = c.shape.tile_rows;
-    return window_keys(l.n_cached + tile * tr / group, l.n_cached + (std::min((tile + 1) * tr, rows) - 1) / group, window, n_first);
+    return window_keys(l.n_cached + tile * tr / group, l.n_cached + (std::min((tile + 1) * tr, rows) - 1) / group, window, n_first, c.unit);
   }
   const int64_t tt = c.tile_tokens;
   return window_keys_full_first(l.n_cached + tile * tt, l.n_cached + std::min<int64_t>((tile + 1) * tt, l.n_new) - 1, window, n_first);
@@ -80,6 +81,53 @@ RowsShape few_rows_shape(bool f32, int head_dim, bool single_tokens) {
   return {kFewRows, head_dim <= 64 ? (single_tokens ? 7 : 5) : single_tokens ? 12 : 8, 60, 1};
 }
 
+// Packed rows over an 8-bit pool: a step is 64 keys, a workgroup has four waves and two of them fit a CU.
+RowsShape e4m3_shape(int head_dim, bool large) {
+  const int step = head_dim <= 64 ? 6 : head_dim <= 128 ? 10 : 18;
+  if (large && head_dim <= 128) return {32, step + step / 2, 60, 1};
+  return {kFewRows, step, 60, 1};
+}
+
+void finish_rows(const WindowShape& s, const std::vector<WindowLens>& lens, const Candidate& best, int waves_rows, WindowPlan& out) {
+  const int group = s.n_q_heads / s.n_kv_heads;
+  out.variant = kWindowRows;
+  out.tile_rows = best.shape.tile_rows;
+  out.single_tiles = true;
+  for (const WindowLens& l : lens) out.single_tiles &= (int64_t)l.n_new * group <= best.shape.tile_rows;
+  out.one_launch = out.single_tiles && best.shape.tile_rows == kFewRows;
+  for (const WindowLens& l : lens) out.one_launch &= (int64_t)l.n_new * group <= waves_rows;
+  out.part_rows = (int64_t)s.n_kv_heads * best.shape.tile_rows;
+  out.part_width = s.head_dim <= 64 ? 64 : s.head_dim <= 128 ? 128 : 256;
+}
+
+void add_items(const WindowShape& s, const std::vector<WindowLens>& lens, int32_t window, int32_t n_first, const Candidate& best, WindowPlan& out) {
+  const PlanItems pi = plan_items(best.tiles, best.want, best.params);
+  out.split_tiles = pi.split_tiles;
+  out.items.reserve(pi.items.size());
+  for (const WorkItem& x : pi.items)
+    out.items.push_back({x.req, x.q_tile, x.sub_begin, x.sub_end, x.n_splits, x.first_item,
+                         tile_keys(best, lens[(size_t)x.req], x.q_tile, s.n_q_heads / s.n_kv_heads, window, n_first)});
+}
+
+void plan_window_e4m3(const WindowShape& s, const std::vector<WindowLens>& lens, int32_t window, int32_t n_first, WindowPlan& out) {
+  const int group = s.n_q_heads / s.n_kv_heads;
+  bool few = s.force_tile == 0;
+  for (const WindowLens& l : lens) few &= (int64_t)l.n_new * group <= kFewRows;
+  Candidate best;
+  for (const bool large : {false, true}) {
+    if (large && (few || s.head_dim > 128 || s.force_tile == 1)) break;
+    Candidate c;
+    c.unit = kE4m3Keys;
+    c.shape = e4m3_shape(s.head_dim, large);
+    c.params = rows_plan_params(c.shape, s.n_kv_heads, 2 * s.n_cus, s.force_splits);
+    make_tiles(c, lens, group, window, n_first);
+    c.want = plan_pieces(c.tiles, c.params, kMostSlots / c.shape.slots, &c.cost);
+    if (best.tiles.empty() || (large && s.force_tile == 2) || c.cost.span < best.cost.span) best = std::move(c);
+  }
+  finish_rows(s, lens, best, 4, out);
+  add_items(s, lens, window, n_first, best, out);
+}
+
 }  // namespace
 
 void plan_window(const WindowShape& s, const std::vector<WindowLens>& lens, int32_t window, int32_t n_first, WindowPlan& out) {
@@ -89,6 +137,7 @@ void plan_window(const WindowShape& s, const std::vector<WindowLens>& lens, int3
   int64_t total = 0;
   for (const WindowLens& l : lens) total += l.n_new;
   if (total == 0) return;
+  if (s.e4m3) return plan_window_e4m3(s, lens, window, n_first, out);
 
   // Up to 128-wide heads there is a tiling of 16 rows as well.  Single tokens take it: it leaves the combination of the waves half as long (us a call of
   // one caller, 32 / 16 rows, 32Q/8KV: 4096+1 behind 4096 15.4 / 14.0, 20000+1 behind 16384 23.3 / 20.7), and none of the others is looked at

@@ -17,8 +17,8 @@ struct WindowKeys {
   int32_t first_subs = 0, gap = 0, n = 0;
   int32_t n_full = 0, n_part = 0, edge = 0, n_edge = 0, diag = 0;
 };
-// for rows at positions [pos_min, pos_max]: in the order of the context (packed rows) ...
-WindowKeys window_keys(int64_t pos_min, int64_t pos_max, int32_t window, int32_t n_first);
+// for rows at positions [pos_min, pos_max]: in the order of the context (packed rows; unit: keys of a sub-tile) ...
+WindowKeys window_keys(int64_t pos_min, int64_t pos_max, int32_t window, int32_t n_first, int unit = 32);
 // ... and with those that every row sees in full in front (pipelined kernels)
 WindowKeys window_keys_full_first(int64_t pos_min, int64_t pos_max, int32_t window, int32_t n_first);
 
@@ -47,7 +47,9 @@ struct WindowShape {
   bool f32;
   int head_dim, n_q_heads, n_kv_heads, n_cus;
   int force_splits, force_tile, force_variant;   // test knobs: 0 = automatic
+  bool e4m3 = false;                             // 8-bit pool: packed rows count 64-key steps
 };
+constexpr int kE4m3Keys = 64;            // keys of a step of its packed rows
 void plan_window(const WindowShape& s, const std::vector<WindowLens>& lens, int32_t window, int32_t n_first, WindowPlan& out);
 
 // ---- gathered weights: key tiles of tile_keys tokens, and parts of the rows that see one
