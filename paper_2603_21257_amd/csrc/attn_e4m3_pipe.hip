@@ -1,0 +1,38 @@
+// Attention over a pool of 8-bit floats on the pipelined bodies (attn_pipeline.h, WinPipe8Cfg): 128-wide heads, tiles of many rows.
+#include "attn_merge.h"
+#include "attn_pipeline.h"
+
+namespace calvo {
+namespace e4m3 {
+
+using namespace attn;
+using Large = WinPipe8Cfg<4, 8, 2>;
+using Small = WinPipe8Cfg<4, 5, 1>;
+
+__global__ void __launch_bounds__(256, 1) __attribute__((amdgpu_num_vgpr(240))) e4m3_pipe_kernel(WinParams p) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  attn_pipeline<Large>(p, smem);
+}
+__global__ void __launch_bounds__(256, 2) __attribute__((amdgpu_num_vgpr(120))) e4m3_duo_kernel(WinParams p) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  attn_pipeline<Small>(p, smem);
+}
+
+}  // namespace e4m3
+
+hipError_t attn_e4m3_pipe_prepare() {
+  const hipError_t e = hipFuncSetAttribute((const void*)e4m3::e4m3_pipe_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, e4m3::Large::LDS_BYTES);
+  if (e != hipSuccess) return e;
+  return hipFuncSetAttribute((const void*)e4m3::e4m3_duo_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, e4m3::Small::LDS_BYTES);
+}
+
+hipError_t launch_attn_e4m3_pipe(const WinParams& p, int variant, int n_items, const int32_t* split_tiles, int n_split_tiles, hipStream_t stream) {
+  if (n_items <= 0) return hipSuccess;
+  const unsigned grid = (unsigned)n_items * (unsigned)(p.n_q_heads / p.heads_per_wg);
+  if (variant == kAttnPipe) hipLaunchKernelGGL(e4m3::e4m3_pipe_kernel, dim3(grid), dim3(256), e4m3::Large::LDS_BYTES, stream, p);
+  else hipLaunchKernelGGL(e4m3::e4m3_duo_kernel, dim3(grid), dim3(256), e4m3::Small::LDS_BYTES, stream, p);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : launch_merge_window(p, split_tiles, n_split_tiles, stream);
+}
+
+}  // namespace calvo

@@ -84,7 +84,10 @@
 // Sub-tiles that touch the causal diagonal or the end of the context are not pipelined: they are at most a handful per
 // workgroup, are requested before the drain of the pipeline and run QK -> mask -> SM -> PV.
 #pragma once
+#include <type_traits>
+
 #include "attn_common.h"
+#include "kv_e4m3.h"
 
 namespace calvo {
 namespace attn {
@@ -103,8 +106,10 @@ struct PipeCfg {
   static constexpr int NI = 8 / NW_;                   // 1 KiB requests per wave, operand and sub-tile
   static constexpr int UNROLL = RING_ % 2 ? 2 * RING_ : RING_;
   static constexpr int PD = 4;         // LDS operand reads run this many operands ahead
+  static constexpr int SLOT = kSlot;
   static constexpr int LDS_BYTES = 2 * RING_ * kSlot;
   static constexpr bool WIN = false;
+  static constexpr bool E8 = false;
   typedef AttnParams Params;
 };
 
@@ -115,6 +120,19 @@ template <int NW_, int RING_, int HB_>
 struct WinPipeCfg : PipeCfg<NW_, RING_, HB_> {
   static constexpr bool WIN = true;
   typedef WinParams Params;
+};
+// Over a pool of 8-bit floats (attn_e4m3_pipe.hip, kv_e4m3.h).  A sub-tile of K or V is half as many bytes, which lie in LDS as they do in the pool, and a
+// ring slot has the scales of its two blocks behind them: a wave's second request of an operand asks for the scale of the block that its first one
+// asks for.  Operands are widened behind the LDS read, four instructions for the eight numbers of a lane, one operand ahead of the MFMAs that take
+// it.  V lies d-major in the pool: a lane's eight keys are four bytes of either block, no transpose read.
+template <int NW_, int RING_, int HB_>
+struct WinPipe8Cfg : WinPipeCfg<NW_, RING_, HB_> {
+  static_assert(NW_ == 4, "a wave requests a quarter of a sub-tile's 4 KiB, and a block's scale");
+  static constexpr int PD = 5;
+  static constexpr int SCALES = 4096;                  // in a slot; 256 bytes for each wave's request
+  static constexpr int SLOT = SCALES + 4 * 256;
+  static constexpr int LDS_BYTES = 2 * RING_ * SLOT;
+  static constexpr bool E8 = true;
 };
 // WIN: the reference of a row that has seen no key.  Finite, so that the weight of a hidden key (score -inf) is 0 against it; far enough below
 // every score for the first visible one to pass the bound.
@@ -132,11 +150,15 @@ __device__ inline void set_m0(unsigned lds_base, int off) {
 __device__ inline void dma_1k_m0(const unsigned char* sbase, unsigned voff) {
   asm volatile("global_load_lds_dwordx4 %0, %1" : : "v"(voff), "s"(sbase));
 }
+// 64 lanes x 4 bytes
+__device__ inline void dma_256_m0(const unsigned char* sbase, unsigned voff) {
+  asm volatile("global_load_lds_dword %0, %1" : : "v"(voff), "s"(sbase));
+}
 // byte offset of a ring slot, for slots known at compile time and for others
-template <int S, int ADD>
-__device__ inline constexpr Tag<S * kSlot + ADD> slot_off(Tag<S>, Tag<ADD>) { return {}; }
-template <int ADD>
-__device__ inline int slot_off(int s, Tag<ADD>) { return s * kSlot + ADD; }
+template <int SLOT, int S, int ADD>
+__device__ inline constexpr Tag<S * SLOT + ADD> slot_off(Tag<S>, Tag<ADD>) { return {}; }
+template <int SLOT, int ADD>
+__device__ inline int slot_off(int s, Tag<ADD>) { return s * SLOT + ADD; }
 template <int V>
 __device__ inline void opaque(Tag<V>&) {}
 __device__ inline void opaque(int& s) { asm volatile("" : "+s"(s)); }
@@ -198,7 +220,11 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   constexpr float kUnset = WIN ? kNoRef : -INFINITY;
   constexpr int NW = Cfg_::NW, HB = Cfg_::HB, QB = Cfg_::QB, RING = Cfg_::RING, KA = Cfg_::KA, VA = Cfg_::VA, NI = Cfg_::NI, PD = Cfg_::PD;
   constexpr bool ACC = HB == 2;
-  constexpr int kVBase = RING * kSlot;                 // V ring follows the K ring
+  constexpr bool E8 = Cfg_::E8;
+  constexpr int SLOT = Cfg_::SLOT;
+  constexpr int kVBase = RING * SLOT;                  // V ring follows the K ring
+  constexpr int kRow = E8 ? 128 : attn::kRow;          // bytes of a key of one head in LDS
+  typedef typename std::conditional<E8, u32x2, bf16x8>::type raw_t;      // an operand as it comes out of LDS
   const lds_u8* lds = (const lds_u8*)smem;
   const unsigned lds0 = (unsigned)(size_t)lds;
   const int tid = threadIdx.x;
@@ -268,13 +294,24 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   const unsigned half_b = kBlockTokens * row_b;
   const int brow0 = (32 / NW) * (wave % (NW / 2)) + (lane >> 4);
   unsigned voff_k[NI], voff_v[NI];
+  if constexpr (E8) {
+    // K's 16-byte chunks are swizzled by the row pair (two rows are a pass over the banks); V is read 256 consecutive bytes at a time
+    const E4m3Block lay = e4m3_block(Hkv, kD);
+    const int row = 8 * (wave & 1) + (lane >> 3);
+    voff_k[0] = kv * lay.tile + row * kRow + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
+    voff_k[1] = lay.scales + 4 * kv;
+    voff_v[0] = lay.v + kv * lay.tile + 1024 * (wave & 1) + 16 * lane;
+    voff_v[1] = lay.scales + 4 * (Hkv + kv);
+  } else {
 #pragma unroll
-  for (int h = 0; h < NI; h++) {
-    const int row = brow0 + 4 * h;
-    voff_k[h] = row * row_b + kv * kRow + (((lane & 15) ^ (row & 15)) << 4);
-    voff_v[h] = half_b + row * row_b + kv * kRow + (((lane & 15) ^ ((row & 7) << 1)) << 4);
+    for (int h = 0; h < NI; h++) {
+      const int row = brow0 + 4 * h;
+      voff_k[h] = row * row_b + kv * kRow + (((lane & 15) ^ (row & 15)) << 4);
+      voff_v[h] = half_b + row * row_b + kv * kRow + (((lane & 15) ^ ((row & 7) << 1)) << 4);
+    }
   }
-  const unsigned dma_lds = lds0 + wave * (1024 * NI);
+  const unsigned dma_lds = lds0 + wave * (E8 ? 1024 : 1024 * NI);
+  const unsigned scale_lds = E8 ? lds0 + Cfg_::SLOT - 1024 + wave * 256 : 0;
 
   auto fetch_off = [&](int j) -> int64_t {
     if constexpr (WIN) return boffs[jb + j < first_subs ? jb + j : jb + j + gap];
@@ -308,12 +345,16 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   // request I of a step: the NI of a K sub-tile, then the NI of a V sub-tile, into their ring slots
   auto request_m0 = [&](auto kslot, auto vslot, auto idx) {
     constexpr int I = decltype(idx)::value;
-    if constexpr (I < NI) set_m0(dma_lds, slot_off(kslot, Tag<I * 1024>{}));
-    else set_m0(dma_lds, slot_off(vslot, Tag<kVBase + (I - NI) * 1024>{}));
+    if constexpr (E8 && I == 1) set_m0(scale_lds, slot_off<SLOT>(kslot, Tag<0>{}));
+    else if constexpr (E8 && I == 3) set_m0(scale_lds, slot_off<SLOT>(vslot, Tag<kVBase>{}));
+    else if constexpr (I < NI) set_m0(dma_lds, slot_off<SLOT>(kslot, Tag<I * 1024>{}));
+    else set_m0(dma_lds, slot_off<SLOT>(vslot, Tag<kVBase + (I - NI) * 1024>{}));
   };
   auto request_one = [&](const unsigned char* kbase, const unsigned char* vbase, auto idx) {
     constexpr int I = decltype(idx)::value;
-    if constexpr (I < NI) dma_1k_m0(kbase, voff_k[I]);
+    if constexpr (E8 && I == 1) dma_256_m0(kbase, voff_k[1]);
+    else if constexpr (E8 && I == 3) dma_256_m0(vbase, voff_v[1]);
+    else if constexpr (I < NI) dma_1k_m0(kbase, voff_k[I]);
     else dma_1k_m0(vbase, voff_v[I - NI]);
   };
 
@@ -344,12 +385,34 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   // ---- lane-constant operand addresses inside a slot
   const lds_u8* ka_addr[4];
 #pragma unroll
-  for (int ks = 0; ks < 4; ks++) ka_addr[ks] = lds + c * kRow + (((4 * ks + g) ^ c) << 4);
+  for (int ks = 0; ks < 4; ks++)
+    ka_addr[ks] = lds + c * kRow + (E8 ? (((2 * ks + (g >> 1)) ^ (c >> 1)) << 4) + 8 * (g & 1) : ((4 * ks + g) ^ c) << 4);
   const int v_row = 4 * g + (c >> 2);
   const lds_u8* va_addr[8];
 #pragma unroll
   for (int db = 0; db < 8; db++)
-    va_addr[db] = lds + kVBase + v_row * kRow + ((2 * (db ^ (v_row & 7)) + ((c & 3) >> 1)) << 4) + (c & 1) * 8;
+    va_addr[db] = E8 ? lds + kVBase + 256 * db + 16 * c + 4 * g
+                     : lds + kVBase + v_row * kRow + ((2 * (db ^ (v_row & 7)) + ((c & 3) >> 1)) << 4) + (c & 1) * 8;
+  auto raw_k = [&](const lds_u8* a) -> raw_t {
+    if constexpr (E8) return *(const __attribute__((address_space(3))) u32x2*)a;
+    else return read_k(a);
+  };
+  auto raw_v = [&](const lds_u8* a) -> raw_t {
+    typedef const __attribute__((address_space(3))) unsigned* word;
+    if constexpr (E8) return (u32x2){*(word)a, *(word)(a + 16 * kRow)};
+    else return read_vt(a);
+  };
+  // E8: the scales of a slot's two blocks (V: off = kVBase); two of an operand's eight numbers, in bf16
+  auto read_scales = [&](auto slot, auto off, float (&s)[2]) {
+    typedef const __attribute__((address_space(3))) float* number;
+    const lds_u8* a = lds + value_of(slot_off<SLOT>(slot, Tag<decltype(off)::value + SLOT - 1024>{}));
+    s[0] = *(number)a;
+    s[1] = *(number)(a + 512);
+  };
+  auto widen2 = [&](const u32x2& x, auto part, float s) -> unsigned {
+    constexpr int I = decltype(part)::value;
+    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[I >> 1], s, (I & 1) != 0));
+  };
 
   f32x4 sb[2][2][QB];                                  // [parity][kb][qb]
   bf16x8 pb[2][QB];
@@ -405,17 +468,34 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   // S of N query blocks from QB0 on
   auto qk = [&](int slot, auto qb0, auto&& s) {
     constexpr int QB0 = decltype(qb0)::value, N = sizeof(s[0]) / sizeof(f32x4);
+    float sc[2];
+    if constexpr (E8) read_scales(slot, Tag<0>{}, sc);
 #pragma unroll
-    for (int kb = 0; kb < 2; kb++)
+    for (int kb = 0; kb < 2; kb++) {
+      bf16x8 kw[4];
+      if constexpr (E8) {
+#pragma unroll
+        for (int ks = 0; ks < 4; ks++) {
+          const u32x2 x = raw_k(ka_addr[ks] + 16 * kb * kRow + slot * SLOT);
+          kw[ks] = e4m3::widen(x[0], x[1], sc[kb]);
+          pin(kw[ks]);
+        }
+        mfma_settle();
+#pragma unroll
+        for (int ks = 0; ks < 4; ks++) pin(kw[ks]);
+      }
 #pragma unroll
       for (int ks = 0; ks < 4; ks++) {
-        const bf16x8 ka = read_k(ka_addr[ks] + 16 * kb * kRow + slot * kSlot);
+        bf16x8 ka;
+        if constexpr (E8) ka = kw[ks];
+        else ka = read_k(ka_addr[ks] + 16 * kb * kRow + slot * SLOT);
 #pragma unroll
         for (int q = 0; q < N; q++) {
           if (ks == 0) mfma_first(s[kb][q], ka, qB[QB0 + q][ks]);
           else mfma_next(s[kb][q], ka, qB[QB0 + q][ks]);
         }
       }
+    }
     mfma_settle();
 #pragma unroll
     for (int q = 0; q < N; q++) asm volatile("" : "+v"(s[0][q]), "+v"(s[1][q]));
@@ -428,11 +508,31 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
     acc_ready<ACC>(o);
 #pragma unroll
     for (int q = 0; q < N; q++) pin(pw[q]);
+    float sc[2];
+    if constexpr (E8) read_scales(slot, Tag<kVBase>{}, sc);
 #pragma unroll
-    for (int db = 0; db < 8; db++) {
-      const bf16x8 a = read_vt(va_addr[db] + slot * kSlot);
+    for (int d0 = 0; d0 < 8; d0 += 4) {
+      bf16x8 vw[4];
+      if constexpr (E8) {
 #pragma unroll
-      for (int q = 0; q < N; q++) mfma_acc<ACC>(o[db][QB0 + q], a, pw[q]);
+        for (int i = 0; i < 4; i++) {
+          const u32x2 x = raw_v(va_addr[d0 + i] + slot * SLOT);
+          vw[i] = __builtin_bit_cast(bf16x8, (u32x4){widen2(x, Tag<0>{}, sc[0]), widen2(x, Tag<1>{}, sc[0]), widen2(x, Tag<2>{}, sc[1]), widen2(x, Tag<3>{}, sc[1])});
+          pin(vw[i]);
+        }
+        mfma_settle();
+#pragma unroll
+        for (int i = 0; i < 4; i++) pin(vw[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const int db = d0 + i;
+        bf16x8 a;
+        if constexpr (E8) a = vw[i];
+        else a = read_vt(va_addr[db] + slot * SLOT);
+#pragma unroll
+        for (int q = 0; q < N; q++) mfma_acc<ACC>(o[db][QB0 + q], a, pw[q]);
+      }
     }
   };
   auto qk_all = [&](int slot, f32x4 (&s)[2][QB]) { qk(slot, Tag<0>{}, s); };
@@ -440,13 +540,16 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   auto pv_all = [&](int slot, bf16x8 (&pw)[QB]) { pv(slot, Tag<0>{}, Tag<QB>{}, pw); };
 
   // operand i of a step: K operand (key block i%2, d slice i/2) for i < 8, V^T operand of d block i - 8 beyond
-  auto load_opnd = [&](auto idx, auto ks, auto vs) -> bf16x8 {
+  auto load_opnd = [&](auto idx, auto ks, auto vs) -> raw_t {
     constexpr int i = decltype(idx)::value, k = i & 7;
-    if constexpr (i >= 8) return read_vt(va_addr[k] + value_of(slot_off(vs, Tag<0>{})));
-    else return read_k(ka_addr[k >> 1] + value_of(slot_off(ks, Tag<16 * (k & 1) * kRow>{})));
+    if constexpr (i >= 8) return raw_v(va_addr[k] + value_of(slot_off<SLOT>(vs, Tag<0>{})));
+    else return raw_k(ka_addr[k >> 1] + value_of(slot_off<SLOT>(ks, Tag<16 * (k & 1) * kRow>{})));
   };
   auto ring_slot = [](int j) { return (int)((unsigned)j % (unsigned)RING); };
-  bf16x8 pre[PD];
+  raw_t pre[PD];
+  // E8: the first operand of the next step, widened, and the scales of its K
+  u32x4 pre_wide;
+  float pre_scale[2];
 
   // ---- steady step t in ring slot TR: QK(t+1), SM(t), PV(t-1); requests K and V of t + LA from base
   auto step = [&](auto par, auto&& slot, const unsigned char* kbase, const unsigned char* vbase) {
@@ -464,7 +567,29 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
     const bf16x8 (&pp)[QB] = pb[C ^ 1];
     u32x4 pn[QB];
     float x[2], ps[QB], w[2];
-    bf16x8 op[16 + PD];
+    raw_t op[16 + PD];
+    u32x4 wide[17];                                      // E8: operand i in bf16, made in group i - 1
+    float sk[2], skn[2], sv[2];                          // E8: scales of K(t+1), K(t+2), V(t-1)
+    if constexpr (E8) {
+      wide[0] = pre_wide;
+      sk[0] = pre_scale[0];
+      sk[1] = pre_scale[1];
+    }
+    auto widen_part = [&](auto idx, auto part) {
+      constexpr int i = decltype(idx)::value, n = decltype(part)::value;
+      float s;
+      if constexpr (i >= 16) s = skn[i & 1];
+      else if constexpr (i >= 8) s = sv[n >> 1];
+      else s = sk[i & 1];
+      unsigned x = widen2(op[i], part, s);
+      pin(x);
+      wide[i][n] = x;
+    };
+    auto operand = [&](auto idx) -> bf16x8 {
+      constexpr int i = decltype(idx)::value;
+      if constexpr (E8) return __builtin_bit_cast(bf16x8, wide[i]);
+      else return op[i];
+    };
     static_for<0, PD>([&](auto idx) { op[decltype(idx)::value] = pre[decltype(idx)::value]; });
     static_for<0, 16>([&](auto idx) {
       constexpr int i = decltype(idx)::value, k = i & 7;
@@ -476,9 +601,9 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
         // four MFMAs per pair of weights: query block, key block and row of the pair
         constexpr int n = i * QB + qb, pair = n >> 2, part = n & 3, wq = pair >> 2, wkb = (pair >> 1) & 1, wr = 2 * (pair & 1);
         constexpr int qm = i & 1 ? QB - 1 - qb : qb;                  // there and back: either A or B stays from one MFMA to the next
-        if constexpr (i >= 8) mfma_acc<ACC>(o[k][qm], op[i], pp[qm]);
-        else if constexpr (ks == 0) mfma_first(sn[kb][qm], op[i], qB[qm][ks]);
-        else mfma_next(sn[kb][qm], op[i], qB[qm][ks]);
+        if constexpr (i >= 8) mfma_acc<ACC>(o[k][qm], operand(idx), pp[qm]);
+        else if constexpr (ks == 0) mfma_first(sn[kb][qm], operand(idx), qB[qm][ks]);
+        else mfma_next(sn[kb][qm], operand(idx), qB[qm][ks]);
         __builtin_amdgcn_sched_barrier(0);
         // what is free behind an MFMA
         if constexpr (qb == 0) {
@@ -487,7 +612,17 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
         }
         if constexpr (rq_on && qb == QB / 2 - 1) request_m0(KR, VR, Tag<rq>{});
         if constexpr (rq_on && qb == QB / 2) request_one(kbase, vbase, Tag<rq>{});
-        if constexpr (qb == QB - 1 && i < 15) pin(op[i + 1]);         // its wait goes here
+        if constexpr (E8) {
+          if constexpr (qb == QB - 1 && i == 2) read_scales(VS, Tag<kVBase>{}, sv);
+          if constexpr (qb == QB - 1 && i == 9) read_scales(KN, Tag<0>{}, skn);
+          __builtin_amdgcn_sched_barrier(0);
+          // the next operand, done at least two instructions ahead of its first MFMA
+          if constexpr (qb == 0) pin(op[i + 1]);
+          if constexpr (QB == 4) widen_part(Tag<i + 1>{}, qtag);
+          else if constexpr (qb == 0) static_for<0, 4>([&](auto part) { widen_part(Tag<i + 1>{}, part); });
+        } else if constexpr (qb == QB - 1 && i < 15) {
+          pin(op[i + 1]);                                             // its wait goes here
+        }
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (part == 0) {
           x[0] = expo(s[wkb][wq][wr], wq);
@@ -509,6 +644,11 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
       });
     });
     static_for<0, PD>([&](auto idx) { pre[decltype(idx)::value] = op[16 + decltype(idx)::value]; });
+    if constexpr (E8) {
+      pre_wide = wide[16];
+      pre_scale[0] = skn[0];
+      pre_scale[1] = skn[1];
+    }
 #pragma unroll
     for (int qb = 0; qb < QB; qb++) pb[C][qb] = __builtin_bit_cast(bf16x8, pn[qb]);
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(max_of(ps) <= kLazyBound)) != 0, 0)) {
@@ -608,6 +748,13 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
       }
       if (t + 2 < n_pipe) {
         static_for<0, PD>([&](auto idx) { pre[decltype(idx)::value] = load_opnd(idx, Tag<2>{}, Tag<0>{}); });
+        if constexpr (E8) {
+          read_scales(Tag<2>{}, Tag<0>{}, pre_scale);
+          pre_wide = __builtin_bit_cast(u32x4, e4m3::widen(pre[0][0], pre[0][1], pre_scale[0]));
+          pin(pre_wide);
+          mfma_settle();
+          pin(pre_wide);
+        }
         constexpr int U = Cfg_::UNROLL;
         const_paramsp ps = (const_paramsp)__builtin_amdgcn_kernarg_segment_ptr();
         SuffixBases sfx{};
@@ -680,10 +827,22 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
       kb = ks + soff;
       vb = vs + soff - half_b;
     }
+    if constexpr (E8) {                                  // past the last block that one again: its scores are hidden
+      const unsigned at = __builtin_amdgcn_readfirstlane(ring_slot(j) * SLOT);
+      dma_1k(scalar_ptr(kb), voff_k[0], dma_lds + at);
+      dma_1k(scalar_ptr(vb), voff_v[0], dma_lds + at + kVBase);
+      set_m0(scale_lds, (int)at);
+      asm volatile("s_nop 0");
+      dma_256_m0(scalar_ptr(kb), voff_k[1]);
+      set_m0(scale_lds, (int)at + kVBase);
+      asm volatile("s_nop 0");
+      dma_256_m0(scalar_ptr(vb), voff_v[1]);
+      return;
+    }
 #pragma unroll
     for (int h = 0; h < NI; h++) {
       const bool live = sub * kSK + wblk * 16 + brow0 + 4 * h < ctx_len;
-      const unsigned l_k = __builtin_amdgcn_readfirstlane(dma_lds + ring_slot(j) * kSlot + h * 1024);
+      const unsigned l_k = __builtin_amdgcn_readfirstlane(dma_lds + ring_slot(j) * SLOT + h * 1024);
       if (live) {
         dma_1k(scalar_ptr(kb), voff_k[h], l_k);
         dma_1k(scalar_ptr(vb), voff_v[h], l_k + kVBase);
@@ -715,7 +874,19 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   // WIN: V of the sub-tile in tail slot j holds an infinity or a NaN (a lane looks at half a row).  The product takes weight 0 times such a
   // V for a NaN, also in rows that do not see the key.
   auto v_not_finite = [&](int j) -> bool {
-    const lds_u8* half_row = lds + kVBase + ring_slot(j) * kSlot + lane * 128;
+    if constexpr (E8) {
+      float sc[2];
+      read_scales(ring_slot(j), Tag<kVBase>{}, sc);
+      unsigned bad = e4m3::not_finite(sc[0]) || e4m3::not_finite(sc[1]) ? 1u : 0u;
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const u32x4 x = *(const __attribute__((address_space(3))) u32x4*)(lds + kVBase + ring_slot(j) * SLOT + 1024 * i + 16 * lane);
+#pragma unroll
+        for (int e = 0; e < 4; e++) bad |= e4m3::nan_bytes(x[e]);
+      }
+      return __builtin_amdgcn_ballot_w64(bad != 0) != 0;
+    }
+    const lds_u8* half_row = lds + kVBase + ring_slot(j) * SLOT + lane * 128;
     unsigned bad = 0;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
@@ -801,12 +972,19 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
           const int b = 2 * sub + (jj & 1), key0 = kBlockTokens * b;
           const int rest = min(kBlockTokens, ctx_len - key0);
           if (rest <= 0) continue;
-          const unsigned char* kp = pool_w + offs[(b & 1) * (n_blk_pad >> 1) + (b >> 1)] + kv * kRow;
-          const unsigned char* kr = kp + (int64_t)min(c, rest - 1) * row_b + 16 * g;
+          const unsigned char* blk = pool_w + offs[(b & 1) * (n_blk_pad >> 1) + (b >> 1)];
+          const unsigned char* kp = blk + kv * (E8 ? 16 * kD : kRow);
+          const unsigned char* kr = kp + (int64_t)min(c, rest - 1) * (E8 ? kRow : row_b) + (E8 ? 8 : 16) * g;
+          const E4m3Block lay = e4m3_block(Hkv, kD);
           bf16x8 kx[4];
 #pragma unroll
           for (int ks = 0; ks < 4; ks++) {
-            kx[ks] = *(const bf16x8*)(kr + 64 * ks);
+            if constexpr (E8) {
+              const u32x2 x = *(const u32x2*)(kr + 32 * ks);
+              kx[ks] = e4m3::widen(x[0], x[1], *(const float*)(blk + lay.scales + 4 * kv));
+            } else {
+              kx[ks] = *(const bf16x8*)(kr + 64 * ks);
+            }
             pin(kx[ks]);
           }
           mfma_settle();
@@ -840,6 +1018,18 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
             const float mine = t & 2 ? (t & 1 ? w[3] : w[2]) : (t & 1 ? w[1] : w[0]);
             const float wk = __shfl(mine, 16 * (t >> 2) + c);
             if (hidden(key0 + t)) continue;
+            if constexpr (E8) {
+              const unsigned char* v8 = kp + lay.v + t;
+              const float sc = *(const float*)(blk + lay.scales + 4 * (Hkv + kv));
+#pragma unroll
+              for (int db = 0; db < 8; db++)
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                  const bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v8[16 * (16 * db + 4 * g + r)], sc, false);
+                  acc[db][r] = __builtin_fmaf(wk, (float)x[0], acc[db][r]);
+                }
+              continue;
+            }
             const unsigned char* vr = kp + half_b + (int64_t)t * row_b + 8 * g;
 #pragma unroll
             for (int db = 0; db < 8; db++) {

@@ -34,11 +34,17 @@ hipError_t attn_window_pipe_prepare() {
 
 hipError_t launch_attn_window_pipe(const WinParams& p, int variant, int n_items, const int32_t* split_tiles, int n_split_tiles, hipStream_t stream) {
   if (n_items <= 0) return hipSuccess;
-  const unsigned groups = (unsigned)(p.n_q_heads / p.heads_per_wg), grid = (unsigned)n_items * groups;
+  const unsigned grid = (unsigned)n_items * (unsigned)(p.n_q_heads / p.heads_per_wg);
   if (variant == kAttnPipe) hipLaunchKernelGGL(window::window_pipe_kernel, dim3(grid), dim3(256), window::Large::LDS_BYTES, stream, p);
   else hipLaunchKernelGGL(window::window_duo_kernel, dim3(grid), dim3(256), window::Small::LDS_BYTES, stream, p);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : launch_merge_window(p, split_tiles, n_split_tiles, stream);
+}
+
+// The pieces of cut tiles that the pipelined kernels left
+hipError_t launch_merge_window(const WinParams& p, const int32_t* split_tiles, int n_split_tiles, hipStream_t stream) {
   if (n_split_tiles > 0) {
-    const unsigned slots = (unsigned)n_split_tiles * groups * (unsigned)p.row_blocks_per_wg;
+    const unsigned slots = (unsigned)n_split_tiles * (unsigned)(p.n_q_heads / p.heads_per_wg) * (unsigned)p.row_blocks_per_wg;
     if (slots * 32u <= pipe::kMergeSingleRows / 2)
       hipLaunchKernelGGL((pipe::merge_splits_kernel<1, 32, WinParams>), dim3(slots * 8u), dim3(256), 0, stream, p, split_tiles);
     else if (slots * 32u <= pipe::kMergeSingleRows)

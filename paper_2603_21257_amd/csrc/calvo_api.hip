@@ -364,6 +364,7 @@ int window_kernels_ready(calvo_ctx* c) {
   const bool f32 = c->cfg.dtype == CALVO_F32;
   if (c->cfg.dtype == CALVO_E4M3) {
     for (const int rows : {16, 32}) HIP_TRY(attn_e4m3_prepare(c->cfg.head_dim, rows));
+    if (c->cfg.head_dim == 128) HIP_TRY(attn_e4m3_pipe_prepare());
     c->window_kernels = true;
     return CALVO_OK;
   }

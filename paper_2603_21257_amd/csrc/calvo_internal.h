@@ -162,8 +162,12 @@ hipError_t launch_attn_window(const WinParams& p, int dtype, int tile_rows, int 
 hipError_t attn_window_pipe_prepare();
 hipError_t launch_attn_window_pipe(const WinParams& p, int variant, int n_items, const int32_t* split_tiles, int n_split_tiles, hipStream_t stream);
 
+// what both launch behind the tiles
+hipError_t launch_merge_window(const WinParams& p, const int32_t* split_tiles, int n_split_tiles, hipStream_t stream);
 // the same over pools of CALVO_E4M3 (attn_e4m3.hip): work items count 64-key steps
 hipError_t attn_e4m3_prepare(int head_dim, int tile_rows);
+hipError_t attn_e4m3_pipe_prepare();
+hipError_t launch_attn_e4m3_pipe(const WinParams& p, int variant, int n_items, const int32_t* split_tiles, int n_split_tiles, hipStream_t stream);
 hipError_t launch_attn_e4m3(const WinParams& p, int tile_rows, int n_items, const int32_t* split_tiles, int n_split_tiles, hipStream_t stream);
 
 // ---- appending new tokens with the rotation by position (kv_append.hip)

@@ -473,7 +473,8 @@ int window_attn(calvo_window* w, int layer, const void* q, const void* k_new, co
   } else {
     p.heads_per_wg = w->plan.heads_per_wg;
     p.row_blocks_per_wg = attn_mfma_row_blocks(w->plan.variant);
-    HIP_TRY(launch_attn_window_pipe(p, w->plan.variant, n_items, d + w->split_at, n_cut, c->s_compute));
+    if (e4m3) HIP_TRY(launch_attn_e4m3_pipe(p, w->plan.variant, n_items, d + w->split_at, n_cut, c->s_compute));
+    else HIP_TRY(launch_attn_window_pipe(p, w->plan.variant, n_items, d + w->split_at, n_cut, c->s_compute));
   }
   return CALVO_OK;
 }

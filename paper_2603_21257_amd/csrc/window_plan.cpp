@@ -81,6 +81,41 @@ RowsShape few_rows_shape(bool f32, int head_dim, bool single_tokens) {
   return {kFewRows, head_dim <= 64 ? (single_tokens ? 7 : 5) : single_tokens ? 12 : 8, 60, 1};
 }
 
+// bf16 arithmetic and 128-wide heads: one of the pipelined kernels in place of the packed rows, of which the replay makes rows_us microseconds
+void choose_pipelined(const WindowShape& s, const std::vector<WindowLens>& lens, int32_t window, int32_t n_first, double rows_us, Candidate& best) {
+  const int group = s.n_q_heads / s.n_kv_heads;
+  const int hw = attn_heads_per_wg(s.n_q_heads, s.n_kv_heads), head_groups = s.n_q_heads / hw;
+  Candidate pipe, duo;
+  for (Candidate* c : {&pipe, &duo}) {
+    c->variant = c == &pipe ? kAttnPipe : kAttnDuo;
+    c->tile_tokens = attn_mfma_tile_tokens(c->variant, hw);
+    c->params = {head_groups, s.n_cus * (8 / attn_mfma_row_blocks(c->variant)), 48, 30, s.force_splits, false, 0, c->variant == kAttnDuo ? s.n_cus : 0};
+    make_tiles(*c, lens, group, window, n_first);
+    c->want = plan_pieces(c->tiles, c->params, kMostSlots / attn_mfma_row_blocks(c->variant), &c->cost);
+  }
+  // What the replays make of a launch, in us: packed rows 3 and 1.2 times their tenths, the pipelined kernels 0.6 to 0.8 a step, the larger tiles
+  // the more the shorter the launch.  us a call of one caller, 32Q/8KV, packed rows / kAttnDuo / kAttnPipe:
+  //   window 1024   4096+1 17.3 / 28.3 / 35.9      4096+64 21.4 / 30.8 / 46.1    4096+256 23.4 / 30.7 / 46.4    4096+1024 59.1 / 36.3 / 50.9
+  //   window 16384  20000+1 24.9 / 26.6 / 30.7     20000+64 51.1 / 37.5 / 47.8   20000+256 142 / 79.1 / 81.1    20000+1024 504 / 250 / 242
+  //   window 256    0+500 20.5 / 20.6 / 31.5       0+2000 71.9 / 32.0 / 39.2     0+8192 253 / 93.5 / 135
+  // Among the pipelined ones the larger tiles read K and V half as often, the smaller ones have two workgroups on a CU whose starts, ends and sub-tiles
+  // outside the steady loop hide each other.  Those sub-tiles grow with the tokens of a tile (64, 128 or 256 at four, two or one query heads to a workgroup):
+  // the sides cross where a list has some two sub-tiles for every token.  kAttnPipe / kAttnDuo, us a call of one caller, 16384+2048 tokens and 0+16384
+  // behind 2048, 4096, 8192, 16384:
+  //   32Q/8KV  76.3 / 76.2  122 / 128   214 / 232   403 / 449      569 / 541   861 / 847    1300 / 1330  1634 / 1710
+  //   16Q/8KV  63.2 / 53.1  86.4 / 83.0 133 / 140   227 / 254      305 / 271   470 / 443    664 / 698    836 / 881
+  //   40Q/8KV  (320 workgroups on 256 CUs: 740 / 622 at 16384)     779 / 717   1138 / 1077  1679 / 1655  2073 / 2130
+  // Short launches are the smaller tiles' (20000+700 behind 4096 71.8 / 71.3, 20000+64 behind 16384 47.8 / 37.5), and so are those that fill the last round
+  // of CUs badly, where a workgroup of the smaller tiles has its CU to itself.
+  constexpr double kSubsPerToken = 1.9, kLongLaunch = 140., kFilled = 0.9;
+  int64_t subs = 0;
+  for (const PlanTile& t : pipe.tiles) subs += t.n_sub;
+  const bool larger = s.force_variant ? s.force_variant == kAttnPipe
+                                      : (double)subs >= kSubsPerToken * pipe.tile_tokens * (double)pipe.tiles.size() && pipe.cost.span >= kLongLaunch &&
+                                            pipe.cost.load >= kFilled * pipe.cost.span && pipe.cost.span <= 1.03 * duo.cost.span;
+  if (s.force_variant || rows_us >= 0.6 * duo.cost.span) best = std::move(larger ? pipe : duo);
+}
+
 // Packed rows over an 8-bit pool: a step is 64 keys, a workgroup has four waves and two of them fit a CU.
 RowsShape e4m3_shape(int head_dim, bool large) {
   const int step = head_dim <= 64 ? 6 : head_dim <= 128 ? 10 : 18;
@@ -88,25 +123,31 @@ RowsShape e4m3_shape(int head_dim, bool large) {
   return {kFewRows, step, 60, 1};
 }
 
-void finish_rows(const WindowShape& s, const std::vector<WindowLens>& lens, const Candidate& best, int waves_rows, WindowPlan& out) {
+// The launch of the chosen candidate; a packed-rows workgroup merges at most merge_rows rows along (plan_window)
+void make_plan(const WindowShape& s, const std::vector<WindowLens>& lens, int32_t window, int32_t n_first, const Candidate& best, int merge_rows, WindowPlan& out) {
   const int group = s.n_q_heads / s.n_kv_heads;
-  out.variant = kWindowRows;
-  out.tile_rows = best.shape.tile_rows;
-  out.single_tiles = true;
-  for (const WindowLens& l : lens) out.single_tiles &= (int64_t)l.n_new * group <= best.shape.tile_rows;
-  out.one_launch = out.single_tiles && best.shape.tile_rows == kFewRows;
-  for (const WindowLens& l : lens) out.one_launch &= (int64_t)l.n_new * group <= waves_rows;
-  out.part_rows = (int64_t)s.n_kv_heads * best.shape.tile_rows;
-  out.part_width = s.head_dim <= 64 ? 64 : s.head_dim <= 128 ? 128 : 256;
-}
-
-void add_items(const WindowShape& s, const std::vector<WindowLens>& lens, int32_t window, int32_t n_first, const Candidate& best, WindowPlan& out) {
+  const int hw = attn_heads_per_wg(s.n_q_heads, s.n_kv_heads), head_groups = s.n_q_heads / hw;
+  out.variant = best.variant;
+  out.heads_per_wg = hw;
+  if (best.variant == kWindowRows) {
+    out.tile_rows = best.shape.tile_rows;
+    out.single_tiles = true;
+    for (const WindowLens& l : lens) out.single_tiles &= (int64_t)l.n_new * group <= best.shape.tile_rows;
+    out.one_launch = out.single_tiles && best.shape.tile_rows == kFewRows;
+    for (const WindowLens& l : lens) out.one_launch &= (int64_t)l.n_new * group <= merge_rows;
+    out.part_rows = (int64_t)s.n_kv_heads * best.shape.tile_rows;
+    out.part_width = s.head_dim <= 64 ? 64 : s.head_dim <= 128 ? 128 : 256;
+  } else {
+    out.tile_tokens = best.tile_tokens;
+    out.part_rows = (int64_t)head_groups * attn_mfma_row_blocks(best.variant) * 32;
+    out.part_width = 128;
+  }
   const PlanItems pi = plan_items(best.tiles, best.want, best.params);
   out.split_tiles = pi.split_tiles;
   out.items.reserve(pi.items.size());
   for (const WorkItem& x : pi.items)
     out.items.push_back({x.req, x.q_tile, x.sub_begin, x.sub_end, x.n_splits, x.first_item,
-                         tile_keys(best, lens[(size_t)x.req], x.q_tile, s.n_q_heads / s.n_kv_heads, window, n_first)});
+                         tile_keys(best, lens[(size_t)x.req], x.q_tile, group, window, n_first)});
 }
 
 void plan_window_e4m3(const WindowShape& s, const std::vector<WindowLens>& lens, int32_t window, int32_t n_first, WindowPlan& out) {
@@ -124,8 +165,8 @@ void plan_window_e4m3(const WindowShape& s, const std::vector<WindowLens>& lens,
     c.want = plan_pieces(c.tiles, c.params, kMostSlots / c.shape.slots, &c.cost);
     if (best.tiles.empty() || (large && s.force_tile == 2) || c.cost.span < best.cost.span) best = std::move(c);
   }
-  finish_rows(s, lens, best, 4, out);
-  add_items(s, lens, window, n_first, best, out);
+  if (s.head_dim == 128 && s.force_variant != 5 && !few) choose_pipelined(s, lens, window, n_first, 3. + 0.12 * best.cost.span, best);
+  make_plan(s, lens, window, n_first, best, 4, out);
 }
 
 }  // namespace
@@ -133,7 +174,6 @@ void plan_window_e4m3(const WindowShape& s, const std::vector<WindowLens>& lens,
 void plan_window(const WindowShape& s, const std::vector<WindowLens>& lens, int32_t window, int32_t n_first, WindowPlan& out) {
   out = WindowPlan();
   const int group = s.n_q_heads / s.n_kv_heads;
-  const int hw = attn_heads_per_wg(s.n_q_heads, s.n_kv_heads), head_groups = s.n_q_heads / hw;
   int64_t total = 0;
   for (const WindowLens& l : lens) total += l.n_new;
   if (total == 0) return;
@@ -164,62 +204,12 @@ void plan_window(const WindowShape& s, const std::vector<WindowLens>& lens, int3
     c.want = plan_pieces(c.tiles, c.params, kMostSlots / c.shape.slots, &c.cost);
     if (best.tiles.empty() || (kind == 2 && s.force_tile == 2) || 2. * c.cost.span + c.cost.load < 0.97 * (2. * best.cost.span + best.cost.load)) best = std::move(c);
   }
-  if (!s.f32 && s.head_dim == 128 && s.force_variant != 5 && !few) {
-    Candidate pipe, duo;
-    for (Candidate* c : {&pipe, &duo}) {
-      c->variant = c == &pipe ? kAttnPipe : kAttnDuo;
-      c->tile_tokens = attn_mfma_tile_tokens(c->variant, hw);
-      c->params = {head_groups, s.n_cus * (8 / attn_mfma_row_blocks(c->variant)), 48, 30, s.force_splits, false, 0, c->variant == kAttnDuo ? s.n_cus : 0};
-      make_tiles(*c, lens, group, window, n_first);
-      c->want = plan_pieces(c->tiles, c->params, kMostSlots / attn_mfma_row_blocks(c->variant), &c->cost);
-    }
-    // What the replays make of a launch, in us: packed rows 3 and 1.2 times their tenths, the pipelined kernels 0.6 to 0.8 a step, the larger tiles
-    // the more the shorter the launch.  us a call of one caller, 32Q/8KV, packed rows / kAttnDuo / kAttnPipe:
-    //   window 1024   4096+1 17.3 / 28.3 / 35.9      4096+64 21.4 / 30.8 / 46.1    4096+256 23.4 / 30.7 / 46.4    4096+1024 59.1 / 36.3 / 50.9
-    //   window 16384  20000+1 24.9 / 26.6 / 30.7     20000+64 51.1 / 37.5 / 47.8   20000+256 142 / 79.1 / 81.1    20000+1024 504 / 250 / 242
-    //   window 256    0+500 20.5 / 20.6 / 31.5       0+2000 71.9 / 32.0 / 39.2     0+8192 253 / 93.5 / 135
-    // Among the pipelined ones the larger tiles read K and V half as often, the smaller ones have two workgroups on a CU whose starts, ends and sub-tiles
-    // outside the steady loop hide each other.  Those sub-tiles grow with the tokens of a tile (64, 128 or 256 at four, two or one query heads to a workgroup):
-    // the sides cross where a list has some two sub-tiles for every token.  kAttnPipe / kAttnDuo, us a call of one caller, 16384+2048 tokens and 0+16384
-    // behind 2048, 4096, 8192, 16384:
-    //   32Q/8KV  76.3 / 76.2  122 / 128   214 / 232   403 / 449      569 / 541   861 / 847    1300 / 1330  1634 / 1710
-    //   16Q/8KV  63.2 / 53.1  86.4 / 83.0 133 / 140   227 / 254      305 / 271   470 / 443    664 / 698    836 / 881
-    //   40Q/8KV  (320 workgroups on 256 CUs: 740 / 622 at 16384)     779 / 717   1138 / 1077  1679 / 1655  2073 / 2130
-    // Short launches are the smaller tiles' (20000+700 behind 4096 71.8 / 71.3, 20000+64 behind 16384 47.8 / 37.5), and so are those that fill the last round
-    // of CUs badly, where a workgroup of the smaller tiles has its CU to itself.
-    constexpr double kSubsPerToken = 1.9, kLongLaunch = 140., kFilled = 0.9;
-    int64_t subs = 0;
-    for (const PlanTile& t : pipe.tiles) subs += t.n_sub;
-    const bool larger = s.force_variant ? s.force_variant == kAttnPipe
-                                        : (double)subs >= kSubsPerToken * pipe.tile_tokens * (double)pipe.tiles.size() && pipe.cost.span >= kLongLaunch &&
-                                              pipe.cost.load >= kFilled * pipe.cost.span && pipe.cost.span <= 1.03 * duo.cost.span;
-    if (s.force_variant || 3. + 0.12 * best.cost.span >= 0.6 * duo.cost.span) best = std::move(larger ? pipe : duo);
-  }
-  out.variant = best.variant;
-  out.heads_per_wg = hw;
-  if (best.variant == kWindowRows) {
-    out.tile_rows = best.shape.tile_rows;
-    out.single_tiles = true;
-    for (const WindowLens& l : lens) out.single_tiles &= (int64_t)l.n_new * group <= best.shape.tile_rows;
-    // At most one row for each wave of a workgroup: then the last piece of a tile merges them (attn_rows_body.h).  us a call of one caller, by a launch
-    // behind / by the last piece: bf16 D = 128, 32Q/8KV, 4096+1 behind 1024 10.9 / 8.9, four such requests 11.5 / 9.2, 64Q/8KV 12.4 / 12.3 behind 4096; 32Q/4KV
-    // 11.6 / 12.0; D = 64, 16Q/4KV 11.6 / 9.6; D = 256, 16Q/4KV 14.4 / 14.5, 8Q/8KV 15.0 / 14.7; fp32 D = 128, 32Q/8KV 15.0 / 14.8, 32Q/4KV 13.9 / 14.0.  Two rows
-    // a wave and more: 64Q/4KV 12.5 / 16.9, 16Q/1KV 11.7 / 15.9, D = 256 32Q/4KV 14.4 / 20.4, 64Q/4KV 15.1 / 30.4.
-    out.one_launch = out.single_tiles && best.shape.tile_rows == kFewRows;
-    for (const WindowLens& l : lens) out.one_launch &= (int64_t)l.n_new * group <= (s.head_dim <= 128 ? 8 : 4);
-    out.part_rows = (int64_t)s.n_kv_heads * best.shape.tile_rows;
-    out.part_width = s.head_dim <= 64 ? 64 : s.head_dim <= 128 ? 128 : 256;
-  } else {
-    out.tile_tokens = best.tile_tokens;
-    out.part_rows = (int64_t)head_groups * attn_mfma_row_blocks(best.variant) * 32;
-    out.part_width = 128;
-  }
-  const PlanItems pi = plan_items(best.tiles, best.want, best.params);
-  out.split_tiles = pi.split_tiles;
-  out.items.reserve(pi.items.size());
-  for (const WorkItem& x : pi.items)
-    out.items.push_back({x.req, x.q_tile, x.sub_begin, x.sub_end, x.n_splits, x.first_item,
-                         tile_keys(best, lens[(size_t)x.req], x.q_tile, group, window, n_first)});
+  if (!s.f32 && s.head_dim == 128 && s.force_variant != 5 && !few) choose_pipelined(s, lens, window, n_first, 3. + 0.12 * best.cost.span, best);
+  // At most one row for each wave of a workgroup: then the last piece of a tile merges them (attn_rows_body.h).  us a call of one caller, by a launch
+  // behind / by the last piece: bf16 D = 128, 32Q/8KV, 4096+1 behind 1024 10.9 / 8.9, four such requests 11.5 / 9.2, 64Q/8KV 12.4 / 12.3 behind 4096; 32Q/4KV
+  // 11.6 / 12.0; D = 64, 16Q/4KV 11.6 / 9.6; D = 256, 16Q/4KV 14.4 / 14.5, 8Q/8KV 15.0 / 14.7; fp32 D = 128, 32Q/8KV 15.0 / 14.8, 32Q/4KV 13.9 / 14.0.  Two rows
+  // a wave and more: 64Q/4KV 12.5 / 16.9, 16Q/1KV 11.7 / 15.9, D = 256 32Q/4KV 14.4 / 20.4, 64Q/4KV 15.1 / 30.4.
+  make_plan(s, lens, window, n_first, best, s.head_dim <= 128 ? 8 : 4, out);
 }
 
 // Rows that a workgroup takes at least: below, its start and the addition of the parts cost more than the rows

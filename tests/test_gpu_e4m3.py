@@ -52,6 +52,27 @@ def test_long_context(dim):
     run_and_check(Case8([(3000, 150)], 8, 2, dim, seed=5), FULL, 0)
 
 
+# CALVO_ATTN_VARIANT: 64 or 32 query rows per wave in the pipelined kernels, 5 the packed rows
+@pytest.mark.parametrize("variant", ["3", "4", "5"])
+@pytest.mark.parametrize("hq,hkv", [(8, 2), (32, 8), (5, 1), (4, 2)])
+@pytest.mark.parametrize("pieces", ["0", "2", "7"])
+def test_kernels_of_128_wide_heads(variant, hq, hkv, pieces, monkeypatch):
+    monkeypatch.setenv("CALVO_ATTN_VARIANT", variant)
+    if pieces != "0":
+        monkeypatch.setenv("CALVO_ATTN_SPLITS", pieces)
+    for window, n_first in WINDOWS:
+        for i, lens in enumerate([[(0, 1), (17, 3)], [(100, 1), (0, 33), (257, 70), (31, 2)], [(433, 130), (1200, 65)]]):
+            run_and_check(Case8(lens, hq, hkv, 128, seed=300 + i), window, n_first)
+
+
+@pytest.mark.parametrize("variant", ["3", "4", "5"])
+def test_long_contexts_of_128_wide_heads(variant, monkeypatch):
+    """The steady loop with and without whole sub-tiles of first tokens in front."""
+    monkeypatch.setenv("CALVO_ATTN_VARIANT", variant)
+    for window, n_first in [(1000, 0), (1300, 300), (777, 1), (FULL, 0)]:
+        run_and_check(Case8([(6007, 40), (2048, 2)], 8, 2, 128, seed=31), window, n_first)
+
+
 def test_scale():
     c = Case8([(50, 20)], seed=5)
     wh.check_attn(c, c.run(30, 2, scale=0.5), 30, 2, scale=0.5, weight_step=2.0 ** -8)
@@ -65,8 +86,10 @@ def test_large_and_small_values():
         run_and_check(c, FULL, 0)
 
 
-def test_scores_that_grow_along_the_sequence():
-    """The running maximum moves in every step, by a little and by a lot."""
+@pytest.mark.parametrize("variant", ["3", "4", "5"])
+def test_scores_that_grow_along_the_sequence(variant, monkeypatch):
+    """The softmax reference moves in every step, by a little and by a lot."""
+    monkeypatch.setenv("CALVO_ATTN_VARIANT", variant)
     for slope in (0.02, 0.3, -0.3):
         c = Case8([(500, 40)], 8, 2, 128, seed=31)
         k = np.ones((2, 16, 128)) * np.arange(1, 3)[:, None, None]
@@ -85,8 +108,12 @@ def test_scores_that_grow_along_the_sequence():
 @pytest.mark.parametrize("hq,hkv,dim", [(8, 2, 128), (6, 2, 64), (4, 1, 256), (6, 3, 96)])
 @pytest.mark.parametrize("what", ["k byte", "v byte", "both", "scale nan", "scale inf"])
 @pytest.mark.parametrize("pieces", ["0", "3"])
-def test_hidden_keys_do_not_reach_a_row(hq, hkv, dim, what, pieces, monkeypatch):
+@pytest.mark.parametrize("variant", ["3", "4", "5"])
+def test_hidden_keys_do_not_reach_a_row(hq, hkv, dim, what, pieces, variant, monkeypatch):
+    if variant != "5" and dim != 128:
+        pytest.skip("one kernel only")
     monkeypatch.setenv("CALVO_ATTN_SPLITS", pieces)
+    monkeypatch.setenv("CALVO_ATTN_VARIANT", variant)
     c = Case8([(150, 90)], hq, hkv, dim, seed=11)
     n8, t = c.hkv * 16 * dim, c.tables[0]
     window, n_first = 40, 5
