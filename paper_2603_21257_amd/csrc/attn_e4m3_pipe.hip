@@ -7,9 +7,9 @@ namespace e4m3 {
 
 using namespace attn;
 using Large = WinPipe8Cfg<4, 8, 2>;
-using Small = WinPipe8Cfg<4, 5, 1>;
+using Small = WinPipe8Cfg<4, 4, 1>;
 
-__global__ void __launch_bounds__(256, 1) __attribute__((amdgpu_num_vgpr(240))) e4m3_pipe_kernel(WinParams p) {
+__global__ void __launch_bounds__(256, 1) __attribute__((amdgpu_num_vgpr(256))) e4m3_pipe_kernel(WinParams p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   attn_pipeline<Large>(p, smem);
 }

@@ -84,8 +84,6 @@
 // Sub-tiles that touch the causal diagonal or the end of the context are not pipelined: they are at most a handful per
 // workgroup, are requested before the drain of the pipeline and run QK -> mask -> SM -> PV.
 #pragma once
-#include <type_traits>
-
 #include "attn_common.h"
 #include "kv_e4m3.h"
 
@@ -106,7 +104,6 @@ struct PipeCfg {
   static constexpr int NI = 8 / NW_;                   // 1 KiB requests per wave, operand and sub-tile
   static constexpr int UNROLL = RING_ % 2 ? 2 * RING_ : RING_;
   static constexpr int PD = 4;         // LDS operand reads run this many operands ahead
-  static constexpr int SLOT = kSlot;
   static constexpr int LDS_BYTES = 2 * RING_ * kSlot;
   static constexpr bool WIN = false;
   static constexpr bool E8 = false;
@@ -121,17 +118,17 @@ struct WinPipeCfg : PipeCfg<NW_, RING_, HB_> {
   static constexpr bool WIN = true;
   typedef WinParams Params;
 };
-// Over a pool of 8-bit floats (attn_e4m3_pipe.hip, kv_e4m3.h).  A sub-tile of K or V is half as many bytes, which lie in LDS as they do in the pool, and a
-// ring slot has the scales of its two blocks behind them: a wave's second request of an operand asks for the scale of the block that its first one
-// asks for.  Operands are widened behind the LDS read, four instructions for the eight numbers of a lane, one operand ahead of the MFMAs that take
-// it.  V lies d-major in the pool: a lane's eight keys are four bytes of either block, no transpose read.
+// Over a pool of 8-bit floats (attn_e4m3_pipe.hip, kv_e4m3.h).  Widening two numbers takes the vector ALU 8 cycles, as much as an exponential, and every wave needs
+// all of K and V: they are widened once for the workgroup, on their way from the pool through registers into LDS, not behind every wave's LDS read (sixteen
+// instructions a step and wave instead of 64: 0+16384 tokens 1721 / E8_US us a call).  Step t asks for 16 bytes a lane of K(t + KA) and V(t + VA) and their
+// blocks' scales, and stores K(t + KA - 2) and V(t + VA - 2), asked for two steps before.
+// V lies d-major in the pool and in LDS: a lane's eight keys of an operand are 16 bytes in a row if the k-slot order is slot 8g + 4kb + r <-> key
+// 8g + 4kb + r, so row 4g + r of score tile kb is that key here.  K's chunks are swizzled by the lane that reads the row, V's by d / 4.
 template <int NW_, int RING_, int HB_>
 struct WinPipe8Cfg : WinPipeCfg<NW_, RING_, HB_> {
-  static_assert(NW_ == 4, "a wave requests a quarter of a sub-tile's 4 KiB, and a block's scale");
-  static constexpr int PD = 5;
-  static constexpr int SCALES = 4096;                  // in a slot; 256 bytes for each wave's request
-  static constexpr int SLOT = SCALES + 4 * 256;
-  static constexpr int LDS_BYTES = 2 * RING_ * SLOT;
+  static_assert(NW_ == 4, "a wave takes a quarter of a sub-tile's 4 KiB");
+  static constexpr int KA = (RING_ == 8 ? 4 : 3) + 2;
+  static constexpr int VA = 4;                         // the drain's V is stored by the last steady step
   static constexpr bool E8 = true;
 };
 // WIN: the reference of a row that has seen no key.  Finite, so that the weight of a hidden key (score -inf) is 0 against it; far enough below
@@ -150,15 +147,11 @@ __device__ inline void set_m0(unsigned lds_base, int off) {
 __device__ inline void dma_1k_m0(const unsigned char* sbase, unsigned voff) {
   asm volatile("global_load_lds_dwordx4 %0, %1" : : "v"(voff), "s"(sbase));
 }
-// 64 lanes x 4 bytes
-__device__ inline void dma_256_m0(const unsigned char* sbase, unsigned voff) {
-  asm volatile("global_load_lds_dword %0, %1" : : "v"(voff), "s"(sbase));
-}
 // byte offset of a ring slot, for slots known at compile time and for others
-template <int SLOT, int S, int ADD>
-__device__ inline constexpr Tag<S * SLOT + ADD> slot_off(Tag<S>, Tag<ADD>) { return {}; }
-template <int SLOT, int ADD>
-__device__ inline int slot_off(int s, Tag<ADD>) { return s * SLOT + ADD; }
+template <int S, int ADD>
+__device__ inline constexpr Tag<S * kSlot + ADD> slot_off(Tag<S>, Tag<ADD>) { return {}; }
+template <int ADD>
+__device__ inline int slot_off(int s, Tag<ADD>) { return s * kSlot + ADD; }
 template <int V>
 __device__ inline void opaque(Tag<V>&) {}
 __device__ inline void opaque(int& s) { asm volatile("" : "+s"(s)); }
@@ -221,10 +214,7 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   constexpr int NW = Cfg_::NW, HB = Cfg_::HB, QB = Cfg_::QB, RING = Cfg_::RING, KA = Cfg_::KA, VA = Cfg_::VA, NI = Cfg_::NI, PD = Cfg_::PD;
   constexpr bool ACC = HB == 2;
   constexpr bool E8 = Cfg_::E8;
-  constexpr int SLOT = Cfg_::SLOT;
-  constexpr int kVBase = RING * SLOT;                  // V ring follows the K ring
-  constexpr int kRow = E8 ? 128 : attn::kRow;          // bytes of a key of one head in LDS
-  typedef typename std::conditional<E8, u32x2, bf16x8>::type raw_t;      // an operand as it comes out of LDS
+  constexpr int kVBase = RING * kSlot;                 // V ring follows the K ring
   const lds_u8* lds = (const lds_u8*)smem;
   const unsigned lds0 = (unsigned)(size_t)lds;
   const int tid = threadIdx.x;
@@ -294,24 +284,52 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   const unsigned half_b = kBlockTokens * row_b;
   const int brow0 = (32 / NW) * (wave % (NW / 2)) + (lane >> 4);
   unsigned voff_k[NI], voff_v[NI];
-  if constexpr (E8) {
-    // K's 16-byte chunks are swizzled by the row pair (two rows are a pass over the banks); V is read 256 consecutive bytes at a time
-    const E4m3Block lay = e4m3_block(Hkv, kD);
-    const int row = 8 * (wave & 1) + (lane >> 3);
-    voff_k[0] = kv * lay.tile + row * kRow + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
-    voff_k[1] = lay.scales + 4 * kv;
-    voff_v[0] = lay.v + kv * lay.tile + 1024 * (wave & 1) + 16 * lane;
-    voff_v[1] = lay.scales + 4 * (Hkv + kv);
-  } else {
 #pragma unroll
-    for (int h = 0; h < NI; h++) {
-      const int row = brow0 + 4 * h;
-      voff_k[h] = row * row_b + kv * kRow + (((lane & 15) ^ (row & 15)) << 4);
-      voff_v[h] = half_b + row * row_b + kv * kRow + (((lane & 15) ^ ((row & 7) << 1)) << 4);
+  for (int h = 0; h < NI; h++) {
+    const int row = brow0 + 4 * h;
+    voff_k[h] = row * row_b + kv * kRow + (((lane & 15) ^ (row & 15)) << 4);
+    voff_v[h] = half_b + row * row_b + kv * kRow + (((lane & 15) ^ ((row & 7) << 1)) << 4);
+  }
+  const unsigned dma_lds = lds0 + wave * (1024 * NI);
+
+  // E8: a lane's 16 bytes of its wave's block, 16 d of a key and 16 keys of a d; where they go, widened
+  const E4m3Block lay = e4m3_block(Hkv, kD);
+  const unsigned raw_at = kv * lay.tile + 1024 * (wave & 1) + 16 * lane, scale_at = lay.scales + 4 * kv;
+  u32x4 raw_k[2], raw_v[2];
+  float raw_ks[2], raw_vs[2];
+  unsigned char *put_k[2], *put_v[2];
+  if constexpr (E8) {
+    const int row = 16 * wblk + 8 * (wave & 1) + (lane >> 3), d = 64 * (wave & 1) + lane;
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      put_k[h] = smem + row * kRow + (((2 * (lane & 7) + h) ^ ((row & 3) | (row >> 3) << 2)) << 4);
+      put_v[h] = smem + kVBase + d * 64 + (((2 * wblk + h) ^ (d >> 2 & 3)) << 4);
     }
   }
-  const unsigned dma_lds = lds0 + wave * (E8 ? 1024 : 1024 * NI);
-  const unsigned scale_lds = E8 ? lds0 + Cfg_::SLOT - 1024 + wave * 256 : 0;
+  auto ask_k = [&](const unsigned char* base, u32x4& x, float& s) {
+    x = *(const u32x4*)(base + raw_at);
+    s = *(const float*)(base + scale_at);
+  };
+  auto ask_v = [&](const unsigned char* base, u32x4& x, float& s) {
+    x = *(const u32x4*)(base + lay.v + raw_at);
+    s = *(const float*)(base + scale_at + 4 * Hkv);
+  };
+  auto widen2 = [&](const u32x4& x, auto part, float s) -> unsigned {
+    constexpr int I = decltype(part)::value;
+    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[I >> 1], s, (I & 1) != 0));
+  };
+  auto put = [&](unsigned char* (&at)[2], int off, const u32x4& x, float s) {
+    static_for<0, 2>([&](auto h) {
+      constexpr int H = decltype(h)::value;
+      *(u32x4*)(at[H] + off) = (u32x4){widen2(x, Tag<4 * H>{}, s), widen2(x, Tag<4 * H + 1>{}, s), widen2(x, Tag<4 * H + 2>{}, s), widen2(x, Tag<4 * H + 3>{}, s)};
+    });
+  };
+  // E8: what the waves have stored to LDS is there for all; loads from the pool stay under way
+  auto meet = [&] {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+  };
 
   auto fetch_off = [&](int j) -> int64_t {
     if constexpr (WIN) return boffs[jb + j < first_subs ? jb + j : jb + j + gap];
@@ -345,16 +363,12 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   // request I of a step: the NI of a K sub-tile, then the NI of a V sub-tile, into their ring slots
   auto request_m0 = [&](auto kslot, auto vslot, auto idx) {
     constexpr int I = decltype(idx)::value;
-    if constexpr (E8 && I == 1) set_m0(scale_lds, slot_off<SLOT>(kslot, Tag<0>{}));
-    else if constexpr (E8 && I == 3) set_m0(scale_lds, slot_off<SLOT>(vslot, Tag<kVBase>{}));
-    else if constexpr (I < NI) set_m0(dma_lds, slot_off<SLOT>(kslot, Tag<I * 1024>{}));
-    else set_m0(dma_lds, slot_off<SLOT>(vslot, Tag<kVBase + (I - NI) * 1024>{}));
+    if constexpr (I < NI) set_m0(dma_lds, slot_off(kslot, Tag<I * 1024>{}));
+    else set_m0(dma_lds, slot_off(vslot, Tag<kVBase + (I - NI) * 1024>{}));
   };
   auto request_one = [&](const unsigned char* kbase, const unsigned char* vbase, auto idx) {
     constexpr int I = decltype(idx)::value;
-    if constexpr (E8 && I == 1) dma_256_m0(kbase, voff_k[1]);
-    else if constexpr (E8 && I == 3) dma_256_m0(vbase, voff_v[1]);
-    else if constexpr (I < NI) dma_1k_m0(kbase, voff_k[I]);
+    if constexpr (I < NI) dma_1k_m0(kbase, voff_k[I]);
     else dma_1k_m0(vbase, voff_v[I - NI]);
   };
 
@@ -385,34 +399,20 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   // ---- lane-constant operand addresses inside a slot
   const lds_u8* ka_addr[4];
 #pragma unroll
-  for (int ks = 0; ks < 4; ks++)
-    ka_addr[ks] = lds + c * kRow + (E8 ? (((2 * ks + (g >> 1)) ^ (c >> 1)) << 4) + 8 * (g & 1) : ((4 * ks + g) ^ c) << 4);
+  for (int ks = 0; ks < 4; ks++) ka_addr[ks] = lds + (E8 ? 8 * (c >> 2) + (c & 3) : c) * kRow + (((4 * ks + g) ^ c) << 4);
+  constexpr int kTileRow = E8 ? 4 : 16;                // rows of K in LDS from score tile 0 to tile 1
   const int v_row = 4 * g + (c >> 2);
   const lds_u8* va_addr[8];
 #pragma unroll
   for (int db = 0; db < 8; db++)
-    va_addr[db] = E8 ? lds + kVBase + 256 * db + 16 * c + 4 * g
+    va_addr[db] = E8 ? lds + kVBase + 1024 * db + 64 * c + ((g ^ (c >> 2)) << 4)
                      : lds + kVBase + v_row * kRow + ((2 * (db ^ (v_row & 7)) + ((c & 3) >> 1)) << 4) + (c & 1) * 8;
-  auto raw_k = [&](const lds_u8* a) -> raw_t {
-    if constexpr (E8) return *(const __attribute__((address_space(3))) u32x2*)a;
-    else return read_k(a);
-  };
-  auto raw_v = [&](const lds_u8* a) -> raw_t {
-    typedef const __attribute__((address_space(3))) unsigned* word;
-    if constexpr (E8) return (u32x2){*(word)a, *(word)(a + 16 * kRow)};
+  auto v_opnd = [&](const lds_u8* a) -> bf16x8 {
+    if constexpr (E8) return read_k(a);
     else return read_vt(a);
   };
-  // E8: the scales of a slot's two blocks (V: off = kVBase); two of an operand's eight numbers, in bf16
-  auto read_scales = [&](auto slot, auto off, float (&s)[2]) {
-    typedef const __attribute__((address_space(3))) float* number;
-    const lds_u8* a = lds + value_of(slot_off<SLOT>(slot, Tag<decltype(off)::value + SLOT - 1024>{}));
-    s[0] = *(number)a;
-    s[1] = *(number)(a + 512);
-  };
-  auto widen2 = [&](const u32x2& x, auto part, float s) -> unsigned {
-    constexpr int I = decltype(part)::value;
-    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[I >> 1], s, (I & 1) != 0));
-  };
+  // key of a lane's score r of tile kb, in its sub-tile
+  auto key_in = [&](int kb, int r) { return E8 ? 8 * g + 4 * kb + r : 16 * kb + 4 * g + r; };
 
   f32x4 sb[2][2][QB];                                  // [parity][kb][qb]
   bf16x8 pb[2][QB];
@@ -468,34 +468,17 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   // S of N query blocks from QB0 on
   auto qk = [&](int slot, auto qb0, auto&& s) {
     constexpr int QB0 = decltype(qb0)::value, N = sizeof(s[0]) / sizeof(f32x4);
-    float sc[2];
-    if constexpr (E8) read_scales(slot, Tag<0>{}, sc);
 #pragma unroll
-    for (int kb = 0; kb < 2; kb++) {
-      bf16x8 kw[4];
-      if constexpr (E8) {
-#pragma unroll
-        for (int ks = 0; ks < 4; ks++) {
-          const u32x2 x = raw_k(ka_addr[ks] + 16 * kb * kRow + slot * SLOT);
-          kw[ks] = e4m3::widen(x[0], x[1], sc[kb]);
-          pin(kw[ks]);
-        }
-        mfma_settle();
-#pragma unroll
-        for (int ks = 0; ks < 4; ks++) pin(kw[ks]);
-      }
+    for (int kb = 0; kb < 2; kb++)
 #pragma unroll
       for (int ks = 0; ks < 4; ks++) {
-        bf16x8 ka;
-        if constexpr (E8) ka = kw[ks];
-        else ka = read_k(ka_addr[ks] + 16 * kb * kRow + slot * SLOT);
+        const bf16x8 ka = read_k(ka_addr[ks] + kTileRow * kb * kRow + slot * kSlot);
 #pragma unroll
         for (int q = 0; q < N; q++) {
           if (ks == 0) mfma_first(s[kb][q], ka, qB[QB0 + q][ks]);
           else mfma_next(s[kb][q], ka, qB[QB0 + q][ks]);
         }
       }
-    }
     mfma_settle();
 #pragma unroll
     for (int q = 0; q < N; q++) asm volatile("" : "+v"(s[0][q]), "+v"(s[1][q]));
@@ -508,31 +491,11 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
     acc_ready<ACC>(o);
 #pragma unroll
     for (int q = 0; q < N; q++) pin(pw[q]);
-    float sc[2];
-    if constexpr (E8) read_scales(slot, Tag<kVBase>{}, sc);
 #pragma unroll
-    for (int d0 = 0; d0 < 8; d0 += 4) {
-      bf16x8 vw[4];
-      if constexpr (E8) {
+    for (int db = 0; db < 8; db++) {
+      const bf16x8 a = v_opnd(va_addr[db] + slot * kSlot);
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const u32x2 x = raw_v(va_addr[d0 + i] + slot * SLOT);
-          vw[i] = __builtin_bit_cast(bf16x8, (u32x4){widen2(x, Tag<0>{}, sc[0]), widen2(x, Tag<1>{}, sc[0]), widen2(x, Tag<2>{}, sc[1]), widen2(x, Tag<3>{}, sc[1])});
-          pin(vw[i]);
-        }
-        mfma_settle();
-#pragma unroll
-        for (int i = 0; i < 4; i++) pin(vw[i]);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        const int db = d0 + i;
-        bf16x8 a;
-        if constexpr (E8) a = vw[i];
-        else a = read_vt(va_addr[db] + slot * SLOT);
-#pragma unroll
-        for (int q = 0; q < N; q++) mfma_acc<ACC>(o[db][QB0 + q], a, pw[q]);
-      }
+      for (int q = 0; q < N; q++) mfma_acc<ACC>(o[db][QB0 + q], a, pw[q]);
     }
   };
   auto qk_all = [&](int slot, f32x4 (&s)[2][QB]) { qk(slot, Tag<0>{}, s); };
@@ -540,16 +503,13 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   auto pv_all = [&](int slot, bf16x8 (&pw)[QB]) { pv(slot, Tag<0>{}, Tag<QB>{}, pw); };
 
   // operand i of a step: K operand (key block i%2, d slice i/2) for i < 8, V^T operand of d block i - 8 beyond
-  auto load_opnd = [&](auto idx, auto ks, auto vs) -> raw_t {
+  auto load_opnd = [&](auto idx, auto ks, auto vs) -> bf16x8 {
     constexpr int i = decltype(idx)::value, k = i & 7;
-    if constexpr (i >= 8) return raw_v(va_addr[k] + value_of(slot_off<SLOT>(vs, Tag<0>{})));
-    else return raw_k(ka_addr[k >> 1] + value_of(slot_off<SLOT>(ks, Tag<16 * (k & 1) * kRow>{})));
+    if constexpr (i >= 8) return v_opnd(va_addr[k] + value_of(slot_off(vs, Tag<0>{})));
+    else return read_k(ka_addr[k >> 1] + value_of(slot_off(ks, Tag<kTileRow * (k & 1) * kRow>{})));
   };
   auto ring_slot = [](int j) { return (int)((unsigned)j % (unsigned)RING); };
-  raw_t pre[PD];
-  // E8: the first operand of the next step, widened, and the scales of its K
-  u32x4 pre_wide;
-  float pre_scale[2];
+  bf16x8 pre[PD];
 
   // ---- steady step t in ring slot TR: QK(t+1), SM(t), PV(t-1); requests K and V of t + LA from base
   auto step = [&](auto par, auto&& slot, const unsigned char* kbase, const unsigned char* vbase) {
@@ -567,28 +527,19 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
     const bf16x8 (&pp)[QB] = pb[C ^ 1];
     u32x4 pn[QB];
     float x[2], ps[QB], w[2];
-    raw_t op[16 + PD];
-    u32x4 wide[17];                                      // E8: operand i in bf16, made in group i - 1
-    float sk[2], skn[2], sv[2];                          // E8: scales of K(t+1), K(t+2), V(t-1)
-    if constexpr (E8) {
-      wide[0] = pre_wide;
-      sk[0] = pre_scale[0];
-      sk[1] = pre_scale[1];
-    }
-    auto widen_part = [&](auto idx, auto part) {
-      constexpr int i = decltype(idx)::value, n = decltype(part)::value;
-      float s;
-      if constexpr (i >= 16) s = skn[i & 1];
-      else if constexpr (i >= 8) s = sv[n >> 1];
-      else s = sk[i & 1];
-      unsigned x = widen2(op[i], part, s);
+    bf16x8 op[16 + PD];
+    u32x4 wide;
+    // E8, of group i: K(t + KA - 2) in the first half, V(t + VA - 2) in the second, a conversion a group, a store every fourth
+    auto stage = [&](auto idx) {
+      constexpr int i = decltype(idx)::value, n = i & 7;
+      unsigned x = i < 8 ? widen2(raw_k[C], Tag<n>{}, raw_ks[C]) : widen2(raw_v[C], Tag<n>{}, raw_vs[C]);
       pin(x);
-      wide[i][n] = x;
+      wide[n & 3] = x;
     };
-    auto operand = [&](auto idx) -> bf16x8 {
-      constexpr int i = decltype(idx)::value;
-      if constexpr (E8) return __builtin_bit_cast(bf16x8, wide[i]);
-      else return op[i];
+    auto stage_put = [&](auto idx) {
+      constexpr int i = decltype(idx)::value, H = (i & 7) >> 2;
+      if constexpr (i < 8) *(u32x4*)(put_k[H] + value_of(slot_off(slot(Tag<KA - 2>{}), Tag<0>{}))) = wide;
+      else *(u32x4*)(put_v[H] + value_of(slot_off(slot(Tag<VA - 2>{}), Tag<0>{}))) = wide;
     };
     static_for<0, PD>([&](auto idx) { op[decltype(idx)::value] = pre[decltype(idx)::value]; });
     static_for<0, 16>([&](auto idx) {
@@ -601,29 +552,26 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
         // four MFMAs per pair of weights: query block, key block and row of the pair
         constexpr int n = i * QB + qb, pair = n >> 2, part = n & 3, wq = pair >> 2, wkb = (pair >> 1) & 1, wr = 2 * (pair & 1);
         constexpr int qm = i & 1 ? QB - 1 - qb : qb;                  // there and back: either A or B stays from one MFMA to the next
-        if constexpr (i >= 8) mfma_acc<ACC>(o[k][qm], operand(idx), pp[qm]);
-        else if constexpr (ks == 0) mfma_first(sn[kb][qm], operand(idx), qB[qm][ks]);
-        else mfma_next(sn[kb][qm], operand(idx), qB[qm][ks]);
+        if constexpr (i >= 8) mfma_acc<ACC>(o[k][qm], op[i], pp[qm]);
+        else if constexpr (ks == 0) mfma_first(sn[kb][qm], op[i], qB[qm][ks]);
+        else mfma_next(sn[kb][qm], op[i], qB[qm][ks]);
         __builtin_amdgcn_sched_barrier(0);
         // what is free behind an MFMA
         if constexpr (qb == 0) {
           if constexpr (i + PD < 16) op[i + PD] = load_opnd(Tag<i + PD>{}, KS, VS);
           else op[i + PD] = load_opnd(Tag<i + PD - 16>{}, KN, VS);
         }
-        if constexpr (rq_on && qb == QB / 2 - 1) request_m0(KR, VR, Tag<rq>{});
-        if constexpr (rq_on && qb == QB / 2) request_one(kbase, vbase, Tag<rq>{});
         if constexpr (E8) {
-          if constexpr (qb == QB - 1 && i == 2) read_scales(VS, Tag<kVBase>{}, sv);
-          if constexpr (qb == QB - 1 && i == 9) read_scales(KN, Tag<0>{}, skn);
-          __builtin_amdgcn_sched_barrier(0);
-          // the next operand, done at least two instructions ahead of its first MFMA
-          if constexpr (qb == 0) pin(op[i + 1]);
-          if constexpr (QB == 4) widen_part(Tag<i + 1>{}, qtag);
-          else if constexpr (qb == 0) static_for<0, 4>([&](auto part) { widen_part(Tag<i + 1>{}, part); });
-        } else if constexpr (qb == QB - 1 && i < 15) {
-          pin(op[i + 1]);                                             // its wait goes here
+          if constexpr (qb == QB - 1 && (i & 3) == 3) stage_put(idx);
+          if constexpr (qb == QB - 1 && i == 7) ask_k(kbase, raw_k[C], raw_ks[C]);
+          if constexpr (qb == QB - 1 && i == 15) ask_v(vbase, raw_v[C], raw_vs[C]);
+        } else {
+          if constexpr (rq_on && qb == QB / 2 - 1) request_m0(KR, VR, Tag<rq>{});
+          if constexpr (rq_on && qb == QB / 2) request_one(kbase, vbase, Tag<rq>{});
         }
+        if constexpr (qb == QB - 1 && i < 15) pin(op[i + 1]);         // its wait goes here
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (E8 && qb == QB / 2 - 1) stage(idx);
         if constexpr (part == 0) {
           x[0] = expo(s[wkb][wq][wr], wq);
           x[1] = expo(s[wkb][wq][wr + 1], wq);
@@ -644,11 +592,6 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
       });
     });
     static_for<0, PD>([&](auto idx) { pre[decltype(idx)::value] = op[16 + decltype(idx)::value]; });
-    if constexpr (E8) {
-      pre_wide = wide[16];
-      pre_scale[0] = skn[0];
-      pre_scale[1] = skn[1];
-    }
 #pragma unroll
     for (int qb = 0; qb < QB; qb++) pb[C][qb] = __builtin_bit_cast(bf16x8, pn[qb]);
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(max_of(ps) <= kLazyBound)) != 0, 0)) {
@@ -671,7 +614,10 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
     // barrier.  One barrier for two steps: at the end of an even step t K up to t + 4 and V up to t + 2, i.e. everything
     // but the requests of the last three steps.  One for each: K up to t + 3 and V up to t, i.e. everything but the requests
     // of the last two steps and those for V before them.
-    if constexpr (!Cfg_::BAR2) {
+    if constexpr (E8) {
+      // K as far as the next steps read is stored before their barrier, and a slot is stored to only behind a barrier that follows its last read
+      if constexpr (!Cfg_::BAR2 || C == 0) meet();
+    } else if constexpr (!Cfg_::BAR2) {
       wait_vm<5 * NI>();
       __syncthreads();
     } else if constexpr (C == 0) {
@@ -706,10 +652,19 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   int t = 0;
   // What the first sub-tile needs comes first: the wait for Q, which the compiler puts in front of the first product, is a
   // wait for every request before it.
+  constexpr int K0 = E8 ? KA - 1 : 0, V0 = E8 ? VA - 1 : 0;            // E8: sub-tiles that are stored before the first steady step
+  u32x4 first_k[K0 + 1], first_v[V0 + 1];
+  float first_ks[K0 + 1], first_vs[V0 + 1];
+  auto pipe_base = [&](int j) { return pool + fetch_off(min(j, n_pipe - 1)); };
   if (n_pipe > 0) {
-    request_k(Tag<0>{});
-    request_v(Tag<0>{});
-    request_k(Tag<1>{});
+    if constexpr (E8) {
+      static_for<0, K0>([&](auto j) { ask_k(pipe_base(decltype(j)::value), first_k[decltype(j)::value], first_ks[decltype(j)::value]); });
+      static_for<0, V0>([&](auto j) { ask_v(pipe_base(decltype(j)::value), first_v[decltype(j)::value], first_vs[decltype(j)::value]); });
+    } else {
+      request_k(Tag<0>{});
+      request_v(Tag<0>{});
+      request_k(Tag<1>{});
+    }
   }
 #pragma unroll
   for (int db = 0; db < 8; db++)
@@ -723,38 +678,48 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
     for (int qb = 0; qb < QB; qb++)
 #pragma unroll
       for (int ks = 0; ks < 4; ks++) pin(qB[qb][ks]);
-    wait_vm<0>();
-    __syncthreads();
+    if constexpr (E8) {
+      static_for<0, K0>([&](auto j) { put(put_k, decltype(j)::value % RING * kSlot, first_k[decltype(j)::value], first_ks[decltype(j)::value]); });
+      static_for<0, V0>([&](auto j) { put(put_v, decltype(j)::value % RING * kSlot, first_v[decltype(j)::value], first_vs[decltype(j)::value]); });
+      // what steps 1 and 2 store
+      ask_k(pipe_base(KA - 1), raw_k[1], raw_ks[1]);
+      ask_v(pipe_base(VA - 1), raw_v[1], raw_vs[1]);
+      ask_k(pipe_base(KA), raw_k[0], raw_ks[0]);
+      ask_v(pipe_base(VA), raw_v[0], raw_vs[0]);
+      meet();
+    } else {
+      wait_vm<0>();
+      __syncthreads();
+    }
     // K(0..K2-1), V(0), V(1): what the first steady steps read.  The rest in the order in which steps would have asked for
     // it, K(j) in front of V(j - KA + VA): the waits of the steady steps count on that order.
     constexpr int K2 = Cfg_::BAR2 ? 5 : 4, DV = KA - VA;
-    static_for<2, K2>([&](auto j) { request_k(j); });
-    static_for<1, K2 - DV>([&](auto j) { request_v(j); });
-    static_for<K2, RING>([&](auto j) {
-      request_k(j);
-      request_v(Tag<decltype(j)::value - DV>{});
-    });
+    if constexpr (!E8) {
+      static_for<2, K2>([&](auto j) { request_k(j); });
+      static_for<1, K2 - DV>([&](auto j) { request_v(j); });
+      static_for<K2, RING>([&](auto j) {
+        request_k(j);
+        request_v(Tag<decltype(j)::value - DV>{});
+      });
+    }
     qk_all(0, sb[0]);
     softmax_all(sb[0], pb[0]);
     t = 1;
     if (n_pipe > 1) {
       qk_all(1, sb[1]);
       // K(0), whose slot is asked for next, is done with
-      wait_vm<((K2 - DV - 2) + 2 * (RING - K2)) * NI>();
-      __syncthreads();
-      if constexpr (KA == RING) {
+      if constexpr (E8) {
+        meet();
+      } else {
+        wait_vm<((K2 - DV - 2) + 2 * (RING - K2)) * NI>();
+        __syncthreads();
+      }
+      if constexpr (!E8 && KA == RING) {
         request_k(Tag<KA>{});
         request_v(Tag<VA>{});
       }
       if (t + 2 < n_pipe) {
         static_for<0, PD>([&](auto idx) { pre[decltype(idx)::value] = load_opnd(idx, Tag<2>{}, Tag<0>{}); });
-        if constexpr (E8) {
-          read_scales(Tag<2>{}, Tag<0>{}, pre_scale);
-          pre_wide = __builtin_bit_cast(u32x4, e4m3::widen(pre[0][0], pre[0][1], pre_scale[0]));
-          pin(pre_wide);
-          mfma_settle();
-          pin(pre_wide);
-        }
         constexpr int U = Cfg_::UNROLL;
         const_paramsp ps = (const_paramsp)__builtin_amdgcn_kernarg_segment_ptr();
         SuffixBases sfx{};
@@ -827,22 +792,10 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
       kb = ks + soff;
       vb = vs + soff - half_b;
     }
-    if constexpr (E8) {                                  // past the last block that one again: its scores are hidden
-      const unsigned at = __builtin_amdgcn_readfirstlane(ring_slot(j) * SLOT);
-      dma_1k(scalar_ptr(kb), voff_k[0], dma_lds + at);
-      dma_1k(scalar_ptr(vb), voff_v[0], dma_lds + at + kVBase);
-      set_m0(scale_lds, (int)at);
-      asm volatile("s_nop 0");
-      dma_256_m0(scalar_ptr(kb), voff_k[1]);
-      set_m0(scale_lds, (int)at + kVBase);
-      asm volatile("s_nop 0");
-      dma_256_m0(scalar_ptr(vb), voff_v[1]);
-      return;
-    }
 #pragma unroll
     for (int h = 0; h < NI; h++) {
       const bool live = sub * kSK + wblk * 16 + brow0 + 4 * h < ctx_len;
-      const unsigned l_k = __builtin_amdgcn_readfirstlane(dma_lds + ring_slot(j) * SLOT + h * 1024);
+      const unsigned l_k = __builtin_amdgcn_readfirstlane(dma_lds + ring_slot(j) * kSlot + h * 1024);
       if (live) {
         dma_1k(scalar_ptr(kb), voff_k[h], l_k);
         dma_1k(scalar_ptr(vb), voff_v[h], l_k + kVBase);
@@ -851,7 +804,23 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
       }
     }
   };
-  constexpr int TG = RING - 2;
+  constexpr int TG = E8 ? 2 : RING - 2;
+  // E8: a group of two sub-tiles on its way in registers
+  auto ask_group = [&](int j0) {
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      const unsigned char* base = pool + boffs[tail_sub(min(j0 + i, n_sub - 1))];
+      ask_k(base, raw_k[i], raw_ks[i]);
+      ask_v(base, raw_v[i], raw_vs[i]);
+    }
+  };
+  auto put_group = [&](int j0) {
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      put(put_k, ring_slot(j0 + i) * kSlot, raw_k[i], raw_ks[i]);
+      put(put_v, ring_slot(j0 + i) * kSlot, raw_v[i], raw_vs[i]);
+    }
+  };
   auto request_group = [&](int j0) {
     for (int j = j0; j < min(n_sub, j0 + TG); j++) request_tail(j);
   };
@@ -859,9 +828,13 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   // ---- drain: PV(t-1), then the one or two sub-tiles that are left; S(t) is in sb[1] (t odd), P(t-1) in pb[0].  The first
   // group of the tail is requested before them: the slots of sub-tiles t and t + 1 are not among its own.
   if (n_pipe > 0) pv_all(ring_slot(t - 1), pb[0]);
-  wait_vm<0>();
-  __syncthreads();
-  request_group(n_pipe);
+  if constexpr (E8) {
+    if (n_pipe < n_sub) ask_group(n_pipe);
+  } else {
+    wait_vm<0>();
+    __syncthreads();
+    request_group(n_pipe);
+  }
   if (t > 0 && t < n_pipe) {
     softmax_all(sb[1], pb[1]);
     pv_all(ring_slot(t), pb[1]);
@@ -874,19 +847,7 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   // WIN: V of the sub-tile in tail slot j holds an infinity or a NaN (a lane looks at half a row).  The product takes weight 0 times such a
   // V for a NaN, also in rows that do not see the key.
   auto v_not_finite = [&](int j) -> bool {
-    if constexpr (E8) {
-      float sc[2];
-      read_scales(ring_slot(j), Tag<kVBase>{}, sc);
-      unsigned bad = e4m3::not_finite(sc[0]) || e4m3::not_finite(sc[1]) ? 1u : 0u;
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        const u32x4 x = *(const __attribute__((address_space(3))) u32x4*)(lds + kVBase + ring_slot(j) * SLOT + 1024 * i + 16 * lane);
-#pragma unroll
-        for (int e = 0; e < 4; e++) bad |= e4m3::nan_bytes(x[e]);
-      }
-      return __builtin_amdgcn_ballot_w64(bad != 0) != 0;
-    }
-    const lds_u8* half_row = lds + kVBase + ring_slot(j) * SLOT + lane * 128;
+    const lds_u8* half_row = lds + kVBase + ring_slot(j) * kSlot + lane * 128;
     unsigned bad = 0;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
@@ -898,12 +859,19 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   };
   bool walk = false;
   for (int j0 = n_pipe; j0 < n_sub; j0 += TG) {
-    if (j0 > n_pipe) {
-      __syncthreads();                                   // everyone has read the group before
-      request_group(j0);
+    if constexpr (E8) {
+      meet();                                            // everyone has read the group before
+      put_group(j0);
+      if (j0 + TG < n_sub) ask_group(j0 + TG);
+      meet();
+    } else {
+      if (j0 > n_pipe) {
+        __syncthreads();                                 // everyone has read the group before
+        request_group(j0);
+      }
+      wait_vm<0>();
+      __syncthreads();
     }
-    wait_vm<0>();
-    __syncthreads();
     for (int j = j0; j < min(n_sub, j0 + TG); j++) {
       const int k0 = tail_sub(j) * kSK;
       if constexpr (WIN) walk |= v_not_finite(j);
@@ -929,7 +897,7 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
               for (int kb = 0; kb < 2; kb++)
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                  const unsigned key = (unsigned)(k0 + 16 * kb + 4 * g + r);
+                  const unsigned key = (unsigned)(k0 + key_in(kb, r));
                   if (!((key - lo < many) | (key < first))) s2[kb][q][r] = -INFINITY;
                 }
             }
@@ -974,14 +942,13 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
           if (rest <= 0) continue;
           const unsigned char* blk = pool_w + offs[(b & 1) * (n_blk_pad >> 1) + (b >> 1)];
           const unsigned char* kp = blk + kv * (E8 ? 16 * kD : kRow);
-          const unsigned char* kr = kp + (int64_t)min(c, rest - 1) * (E8 ? kRow : row_b) + (E8 ? 8 : 16) * g;
-          const E4m3Block lay = e4m3_block(Hkv, kD);
+          const unsigned char* kr = kp + (int64_t)min(c, rest - 1) * (E8 ? (unsigned)kD : row_b) + (E8 ? 8 : 16) * g;
           bf16x8 kx[4];
 #pragma unroll
           for (int ks = 0; ks < 4; ks++) {
             if constexpr (E8) {
               const u32x2 x = *(const u32x2*)(kr + 32 * ks);
-              kx[ks] = e4m3::widen(x[0], x[1], *(const float*)(blk + lay.scales + 4 * kv));
+              kx[ks] = e4m3::widen(x[0], x[1], *(const float*)(blk + scale_at));
             } else {
               kx[ks] = *(const bf16x8*)(kr + 64 * ks);
             }
@@ -1019,13 +986,12 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
             const float wk = __shfl(mine, 16 * (t >> 2) + c);
             if (hidden(key0 + t)) continue;
             if constexpr (E8) {
-              const unsigned char* v8 = kp + lay.v + t;
-              const float sc = *(const float*)(blk + lay.scales + 4 * (Hkv + kv));
+              const float sc = *(const float*)(blk + scale_at + 4 * Hkv);
 #pragma unroll
               for (int db = 0; db < 8; db++)
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                  const bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v8[16 * (16 * db + 4 * g + r)], sc, false);
+                  const bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(kp[lay.v + 16 * (16 * db + 4 * g + r) + t], sc, false);
                   acc[db][r] = __builtin_fmaf(wk, (float)x[0], acc[db][r]);
                 }
               continue;

@@ -14,7 +14,7 @@ def test_pipelined(kernel, mfmas, exps, turns, tmp_path):
     assert re.search(r"VGPRs Spill: 0\b", usage) and re.search(r"ScratchSize \[bytes/lane\]: 0\b", usage), usage
     steady = [x for x in re.split(r"^\.LBB\w+:", asm, flags=re.M) if x.count("v_mfma") == mfmas and x.count("v_exp_f32") == exps]
     assert len(steady) >= turns
-    assert all("v_accvgpr" not in x and x.count("v_cvt_scalef32") == 64 for x in steady)
+    assert all("v_accvgpr" not in x and x.count("v_cvt_scalef32") == 16 for x in steady)
     code = Code(asm, kernel)
     assert sum(x.mfma for x in code.ins) >= turns * mfmas
     assert code.hazards() == []
