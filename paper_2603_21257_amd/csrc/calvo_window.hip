@@ -402,7 +402,7 @@ int kv_append(calvo_window* w, int layer, const void* k_new, int64_t k_stride, c
     for (const Range& a : to)
       for (const Range& b : from)
         if ((rc = apart(a, b)) != CALVO_OK) return rc;
-    if (((int64_t)w->n_touched * ((cf.n_kv_heads + 3) / 4) + w->total) * 256 > kMostThreads) return fail(CALVO_EINVAL, "too many new tokens");
+    if (((int64_t)w->n_touched * ((cf.n_kv_heads + 1) / 2) + w->total) * 256 > kMostThreads) return fail(CALVO_EINVAL, "too many new tokens");
   }
   ON_DEVICE(c);
   if ((rc = queue_behind_layer(c, layer)) != CALVO_OK) return rc;

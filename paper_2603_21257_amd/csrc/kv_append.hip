@@ -14,15 +14,19 @@ using namespace attn;
 using e4m3::bits_of;
 using e4m3::float_of;
 
-// the last request that begins at or before a token (halving: append_suffix, attn_common.h)
-__device__ inline int request_of(const ReqDesc* reqs, int n_reqs, int tok) {
-  int r = 0;
-  for (int end = n_reqs; end - r > 1;) {
-    const int mid = (r + end) / 2;
-    if (tok >= reqs[mid].q_off) r = mid;
-    else end = mid;
+// The last of n requests whose entry is at or below x (entries ascend, the first is): 64 of them at a time, for a whole wave
+template <typename F>
+__device__ inline int last_at_or_below(int n, int x, F&& entry) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0;
+  while (n > 1) {
+    const int stride = (n + 63) / 64, i = lane * stride;
+    const int c = __popcll(__builtin_amdgcn_ballot_w64(i < n && entry(lo + min(i, n - 1)) <= x));
+    const int skip = (c - 1) * stride;
+    lo += skip;
+    n = min(stride, n - skip);
   }
-  return r;
+  return lo;
 }
 
 __device__ inline f32x2 cos_sin(const RopeParams& rope, int pos, int i) {
@@ -57,6 +61,9 @@ struct Chunk<float> {
   static __device__ float one(const unsigned char* row, int d) { return ((const float*)row)[d]; }
   static __device__ u32x4 packed(const float (&x)[4]) { return (u32x4){bits_of(x[0]), bits_of(x[1]), bits_of(x[2]), bits_of(x[3])}; }
 };
+
+// How pairs lie in 16-byte chunks of a row: none is rotated, a pair's elements are in the same places of two chunks, in one chunk, or anywhere
+enum { kNone, kHalves, kNeighbours, kAnywhere };
 
 // Chunk ch of a head's row, rotated.  cs: (cos, sin) of the token's pairs.
 template <typename T>
@@ -94,24 +101,26 @@ __device__ inline void rotated(const RopeParams& rope, const unsigned char* row,
   }
 }
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kMostTokens = 4;       // of a workgroup: one wave finds the place of each
 
 // Rows of tokens [t0, t0 + n): q -> q_out, and where the pool holds the same type k and v -> pool.  cs: room for n * rot / 2 pairs.
 template <typename T, bool KV>
 __device__ inline void move_rows(const KvAppendParams& p, int t0, int n, f32x2* cs) {
   constexpr int N = Chunk<T>::N;
-  const int half = p.rope.half;
-  for (int i = threadIdx.x; i < n * half; i += kThreads) {
-    const int tok = t0 + i / half;
-    int pos;
-    if (p.rope.positions) {
-      pos = p.rope.positions[tok];
-    } else {
-      const ReqDesc rd = p.reqs[request_of(p.reqs, p.n_reqs, tok)];
-      pos = rd.prefix_len + tok - rd.q_off;
+  __shared__ int pos_of[kMostTokens];
+  __shared__ int64_t row_of[kMostTokens];                      // of the pool, in tokens from its first one (K of a block, then its V)
+  const int half = p.rope.half, wave = threadIdx.x >> 6;
+  if (wave < n) {
+    const int tok = t0 + wave;
+    const ReqDesc rd = p.reqs[last_at_or_below(p.n_reqs, tok, [&](int r) { return p.reqs[r].q_off; })];
+    const int pos = rd.prefix_len + (tok - rd.q_off);
+    if ((threadIdx.x & 63) == 0) {
+      pos_of[wave] = p.rope.positions ? p.rope.positions[tok] : pos;
+      if constexpr (KV) row_of[wave] = (int64_t)p.tables[rd.table_off + pos / kBlockTokens] * 2 * kBlockTokens + pos % kBlockTokens;
     }
-    cs[i] = cos_sin(p.rope, pos, i % half);
   }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n * half; i += kThreads) cs[i] = cos_sin(p.rope, pos_of[i / half], i % half);
   __syncthreads();
   const int chunks = p.head_dim / N, row_chunks = p.n_kv_heads * chunks;
   const int nq = p.q ? p.n_q_heads * chunks : 0, nk = KV && p.k ? row_chunks : 0;
@@ -123,11 +132,8 @@ __device__ inline void move_rows(const KvAppendParams& p, int t0, int n, f32x2* 
       rotated<T>(p.rope, (const unsigned char*)p.q + tok * p.q_row + (j / chunks) * p.head_dim * (int)sizeof(T), j % chunks, cs + t * half, x);
       ((u32x4*)p.q_out)[(int64_t)tok * nq + j] = Chunk<T>::packed(x);
     } else if constexpr (KV) {
-      const int r = request_of(p.reqs, p.n_reqs, tok);
-      const ReqDesc rd = p.reqs[r];
-      const int pos = rd.prefix_len + (tok - rd.q_off), k = j - nq;
-      const int64_t slot = p.tables[rd.table_off + pos / kBlockTokens];
-      u32x4* dst = (u32x4*)p.pool_layer + (slot * 2 * kBlockTokens + pos % kBlockTokens) * row_chunks;
+      const int k = j - nq;
+      u32x4* dst = (u32x4*)p.pool_layer + row_of[t] * row_chunks;
       if (k < nk) {
         float x[N];
         rotated<T>(p.rope, (const unsigned char*)p.k + tok * p.k_row + (k / chunks) * p.head_dim * (int)sizeof(T), k % chunks, cs + t * half, x);
@@ -153,10 +159,18 @@ __device__ inline int scale_exponent(unsigned top) {
   if (top >= 0x7f800000u) return 255;
   return max((int)((top + 0x1fffffu) >> 23) - 8, 1);
 }
+// largest of the wave's (of each of 16 lanes by rotations in the vector ALU, then of the four rows)
 __device__ inline unsigned wave_max(unsigned x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = max(x, (unsigned)__shfl_xor((int)x, o));
-  return x;
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x121, 0xf, 0xf, false));   // row_ror:1, 2, 4, 8
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x122, 0xf, 0xf, false));
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xf, 0xf, false));
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, false));
+  unsigned a = x, b = x;
+  row_swap(a, b);
+  a = b = max(a, b);
+  float fa = float_of(a), fb = float_of(b);
+  half_swap(fa, fb);
+  return max(bits_of(fa), bits_of(fb));
 }
 __device__ inline float scale_of(int e) { return e == 255 ? __builtin_nanf("") : float_of((unsigned)e << 23); }
 // four bytes times 2^-shift, rounded
@@ -171,55 +185,100 @@ __device__ inline unsigned rescaled(unsigned x, int shift) {
   return e4m3::pack4(v[0], v[1], v[2], v[3]);
 }
 
-// One (block, head) at a time for a wave.  Tokens [a, e) of the block are new, those in front of a stay (at the larger scale), those behind e become zeros.
-template <int DP>
+// element k of a chunk of bf16
+__device__ inline float number(const u32x4& v, int k) { return float_of(k & 1 ? v[k >> 1] & 0xffff0000u : v[k >> 1] << 16); }
+
+// K or V of one (block, head) for a wave.  Tokens [a, e) of the block are new, those in front of a stay (at the larger scale), those behind e become
+// zeros.  What the block holds is asked for first: it is there when the new values' scale is known.
+template <int DP, int MODE>
 __device__ inline void block_k(const KvAppendParams& p, const unsigned char* src, unsigned char* tile, float* scale, int a, int e, const f32x2* cs) {
   constexpr int NC = DP / 64;                                  // pairs of 8-element chunks that a lane has
-  const int lane = threadIdx.x & 63, t = lane >> 2, D = p.head_dim;
+  const int lane = threadIdx.x & 63, t = lane >> 2, D = p.head_dim, rot = p.rope.rot, half = p.rope.half;
   const bool is_new = t >= a && t < e;
+  const unsigned char* row = src + (t - a) * p.k_row;
+  const f32x2* my_cs = cs + (t - a) * half;
+  const float old_scale = a > 0 ? *scale : 0.f;
+  u32x4 y[NC], own[NC][2], other[NC][2];
   float x[NC][2][8];
+  // all that is asked for, then chunk by chunk: many at a time would need the registers of two waves
+#pragma unroll
+  for (int i = 0; i < NC; i++) {
+    const int d = 64 * i + 16 * (lane & 3);
+    y[i] = (u32x4){0u, 0u, 0u, 0u};
+    if (t < a && d < D) y[i] = *(const u32x4*)(tile + t * D + d);
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      const int d0 = d + 8 * h;
+      own[i][h] = other[i][h] = (u32x4){0u, 0u, 0u, 0u};
+      if (is_new && d < D) {
+        own[i][h] = *(const u32x4*)(row + 2 * d0);
+        if (MODE == kHalves && d0 < rot) other[i][h] = *(const u32x4*)(row + 2 * (d0 < half ? d0 + half : d0 - half));
+      }
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);
   unsigned top = 0;
 #pragma unroll
   for (int i = 0; i < NC; i++)
 #pragma unroll
     for (int h = 0; h < 2; h++) {
-      const int ch = 8 * i + 2 * (lane & 3) + h;
+      const int d0 = 64 * i + 16 * (lane & 3) + 8 * h;
 #pragma unroll
-      for (int k = 0; k < 8; k++) x[i][h][k] = 0.f;
-      if (is_new && 8 * ch < D) rotated<uint16_t>(p.rope, src + (t - a) * p.k_row, ch, cs + (t - a) * p.rope.half, x[i][h]);
+      for (int k = 0; k < 8; k++) x[i][h][k] = number(own[i][h], k);
+      if (MODE != kNone && is_new && d0 < rot) {
+        const bool lower = d0 < half;
+        if constexpr (MODE == kHalves) {
+          const f32x2* c2 = my_cs + (lower ? d0 : d0 - half);
+#pragma unroll
+          for (int k = 0; k < 8; k++) {
+            const float o = number(other[i][h], k);
+            x[i][h][k] = x[i][h][k] * c2[k][0] + (lower ? -o : o) * c2[k][1];
+          }
+        } else if constexpr (MODE == kNeighbours) {
+#pragma unroll
+          for (int k = 0; k < 8; k += 2) {
+            const f32x2 c = my_cs[(d0 + k) >> 1];
+            const float u = x[i][h][k], v = x[i][h][k + 1];
+            x[i][h][k] = u * c[0] - v * c[1];
+            x[i][h][k + 1] = v * c[0] + u * c[1];
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; k++) {
+            const int d = d0 + k;
+            if (d >= rot) continue;
+            const bool first = p.rope.interleaved ? d % 2 == 0 : d < half;
+            const int i2 = p.rope.interleaved ? d / 2 : first ? d : d - half, d2 = p.rope.interleaved ? d ^ 1 : first ? d + half : d - half;
+            const f32x2 c = my_cs[i2];
+            const float o = Chunk<uint16_t>::one(row, d2);
+            x[i][h][k] = x[i][h][k] * c[0] + (first ? -o : o) * c[1];
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      }
 #pragma unroll
       for (int k = 0; k < 8; k++) top = max(top, bits_of(x[i][h][k]) & 0x7fffffffu);
+      __builtin_amdgcn_sched_barrier(0);
     }
-  int ex = scale_exponent(wave_max(top)), before = 0;
-  if (a > 0) {
-    before = (int)(bits_of(*scale) >> 23) & 255;
-    ex = max(ex, before);
-  }
+  const int before = (int)(bits_of(old_scale) >> 23) & 255, ex = max(scale_exponent(wave_max(top)), before);
 #pragma unroll
   for (int i = 0; i < NC; i++) {
     const int d = 64 * i + 16 * (lane & 3);
-    if (d >= D) continue;
-    u32x4* at = (u32x4*)(tile + t * D + d);
-    u32x4 y = {0u, 0u, 0u, 0u};
-    if (ex != 255) {
-      if (is_new) {
+    if (is_new) {
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-          float v[8];
+      for (int h = 0; h < 2; h++) {
+        float v[8];
 #pragma unroll
-          for (int k = 0; k < 8; k++) v[k] = __builtin_amdgcn_ldexpf(x[i][h][k], 127 - ex);
-          y[2 * h] = e4m3::pack4(v[0], v[1], v[2], v[3]);
-          y[2 * h + 1] = e4m3::pack4(v[4], v[5], v[6], v[7]);
-        }
-      } else if (t < a) {
-        y = *at;
-        if (ex != before) {
-#pragma unroll
-          for (int k = 0; k < 4; k++) y[k] = rescaled(y[k], ex - before);
-        }
+        for (int k = 0; k < 8; k++) v[k] = __builtin_amdgcn_ldexpf(x[i][h][k], 127 - ex);
+        y[i][2 * h] = e4m3::pack4(v[0], v[1], v[2], v[3]);
+        y[i][2 * h + 1] = e4m3::pack4(v[4], v[5], v[6], v[7]);
       }
+    } else if (t < a && ex != before) {
+#pragma unroll
+      for (int k = 0; k < 4; k++) y[i][k] = rescaled(y[i][k], ex - before);
     }
-    *at = y;
+    if (ex == 255) y[i] = (u32x4){0u, 0u, 0u, 0u};
+    if (d < D) *(u32x4*)(tile + t * D + d) = y[i];
   }
   if (lane == 0) *scale = scale_of(ex);
 }
@@ -228,8 +287,17 @@ template <int DP>
 __device__ inline void block_v(const KvAppendParams& p, const unsigned char* src, unsigned char* tile, float* scale, int a, int e) {
   constexpr int ND = (DP + 127) / 128;                         // pairs of neighbouring d that a lane has
   const int lane = threadIdx.x & 63, D = p.head_dim;
+  const float old_scale = a > 0 ? *scale : 0.f;
+  u32x4 old[ND][2];
   unsigned x[ND][16];
-  unsigned top = 0;
+#pragma unroll
+  for (int i = 0; i < ND; i++)
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      const int d = 128 * i + 2 * lane;
+      old[i][h] = (u32x4){0u, 0u, 0u, 0u};
+      if (a > 0 && d < D) old[i][h] = *(const u32x4*)(tile + 16 * (d + h));
+    }
 #pragma unroll
   for (int i = 0; i < ND; i++)
 #pragma unroll
@@ -237,46 +305,39 @@ __device__ inline void block_v(const KvAppendParams& p, const unsigned char* src
       const int d = 128 * i + 2 * lane;
       x[i][t] = t >= a && t < e && d < D ? *(const unsigned*)(src + (t - a) * p.v_row + 2 * d) : 0u;
     }
+  unsigned top = 0;
 #pragma unroll
   for (int i = 0; i < ND; i++)
 #pragma unroll
     for (int t = 0; t < 16; t++) top = max(max(top, x[i][t] & 0x7fff0000u), x[i][t] << 16 & 0x7fff0000u);
-  int ex = scale_exponent(wave_max(top)), before = 0;
-  if (a > 0) {
-    before = (int)(bits_of(*scale) >> 23) & 255;
-    ex = max(ex, before);
-  }
+  const int before = (int)(bits_of(old_scale) >> 23) & 255, ex = max(scale_exponent(wave_max(top)), before);
 #pragma unroll
   for (int i = 0; i < ND; i++) {
     const int d = 128 * i + 2 * lane;
     if (d >= D) continue;
 #pragma unroll
     for (int h = 0; h < 2; h++) {
-      u32x4* at = (u32x4*)(tile + 16 * (d + h));
-      u32x4 y = {0u, 0u, 0u, 0u}, old = y;
-      if (a > 0) old = *at;
-      if (ex != 255) {
+      u32x4 y;
 #pragma unroll
-        for (int k = 0; k < 4; k++) {
-          float v[4];
+      for (int k = 0; k < 4; k++) {
+        float v[4];
 #pragma unroll
-          for (int j = 0; j < 4; j++) v[j] = __builtin_amdgcn_ldexpf(float_of(h ? x[i][4 * k + j] & 0xffff0000u : x[i][4 * k + j] << 16), 127 - ex);
-          const unsigned now = e4m3::pack4(v[0], v[1], v[2], v[3]);
-          const int n_old = min(max(a - 4 * k, 0), 4);         // of these four
-          unsigned was = old[k];
-          if (ex != before && n_old) was = rescaled(was, ex - before);
-          const unsigned keep = n_old == 4 ? 0xffffffffu : (1u << 8 * n_old) - 1;
-          y[k] = (was & keep) | (now & ~keep);
-        }
+        for (int j = 0; j < 4; j++) v[j] = __builtin_amdgcn_ldexpf(float_of(h ? x[i][4 * k + j] & 0xffff0000u : x[i][4 * k + j] << 16), 127 - ex);
+        const int n_old = min(max(a - 4 * k, 0), 4);           // of these four
+        unsigned was = old[i][h][k];
+        if (ex != before && n_old) was = rescaled(was, ex - before);
+        const unsigned keep = n_old == 4 ? 0xffffffffu : (1u << 8 * n_old) - 1;
+        y[k] = ex == 255 ? 0u : (was & keep) | (e4m3::pack4(v[0], v[1], v[2], v[3]) & ~keep);
       }
-      *at = y;
+      *(u32x4*)(tile + 16 * (d + h)) = y;
     }
   }
   if (lane == 0) *scale = scale_of(ex);
 }
 
-template <int DP>
-__global__ void __launch_bounds__(kThreads) append_e4m3_kernel(KvAppendParams p, int kv_wgs, int heads_per_wg, int tokens_per_wg) {
+// The workgroups of the first kv_wgs take a touched block and heads_per_wg heads each, a wave K or V of a head at a time; the others rows of q.
+template <int DP, int MODE>
+__global__ void __launch_bounds__(kThreads, (DP > 128 ? 2 : 4) / (MODE == kAnywhere ? 2 : 1)) append_e4m3_kernel(KvAppendParams p, int kv_wgs, int heads_per_wg, int tokens_per_wg) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   f32x2* const cs = (f32x2*)smem;
   if ((int)blockIdx.x >= kv_wgs) {
@@ -286,29 +347,26 @@ __global__ void __launch_bounds__(kThreads) append_e4m3_kernel(KvAppendParams p,
   }
   const int groups = (p.n_kv_heads + heads_per_wg - 1) / heads_per_wg;
   const int blk = blockIdx.x / groups, h0 = (blockIdx.x % groups) * heads_per_wg;
-  int r = 0;                                                   // the last request that writes a block at or before this one
-  for (int end = p.n_reqs; end - r > 1;) {
-    const int mid = (r + end) / 2;
-    if (blk >= p.touched[mid]) r = mid;
-    else end = mid;
-  }
+  const int r = last_at_or_below(p.n_reqs, blk, [&](int i) { return p.touched[i]; });
   const ReqDesc rd = p.reqs[r];
   const int b = rd.prefix_len / kBlockTokens + blk - p.touched[r];
   const int first = max(rd.prefix_len, kBlockTokens * b), a = first - kBlockTokens * b;
   const int e = min(kBlockTokens, rd.prefix_len + rd.suffix_len - kBlockTokens * b);
   const int tok = rd.q_off + first - rd.prefix_len, half = p.rope.half;
-  for (int i = threadIdx.x; i < (e - a) * half; i += kThreads) {
+  const E4m3Block lay = e4m3_block(p.n_kv_heads, p.head_dim);
+  unsigned char* const at = p.pool_layer + (uint64_t)(unsigned)p.tables[rd.table_off + b] * lay.bytes;
+  for (int i = threadIdx.x; MODE != kNone && i < (e - a) * half; i += kThreads) {
     const int t = i / half;
     cs[i] = cos_sin(p.rope, p.rope.positions ? p.rope.positions[tok + t] : first + t, i - t * half);
   }
   __syncthreads();
-  const E4m3Block lay = e4m3_block(p.n_kv_heads, p.head_dim);
-  unsigned char* const at = p.pool_layer + (uint64_t)(unsigned)p.tables[rd.table_off + b] * lay.bytes;
   float* const scales = (float*)(at + lay.scales);
   const unsigned char *k = (const unsigned char*)p.k + tok * p.k_row, *v = (const unsigned char*)p.v + tok * p.v_row;
-  for (int h = h0 + (int)(threadIdx.x >> 6); h < min(h0 + heads_per_wg, p.n_kv_heads); h += kThreads / 64) {
-    block_k<DP>(p, k + 2 * h * p.head_dim, at + h * lay.tile, scales + h, a, e, cs);
-    block_v<DP>(p, v + 2 * h * p.head_dim, at + lay.v + h * lay.tile, scales + p.n_kv_heads + h, a, e);
+  const int units = 2 * (min(h0 + heads_per_wg, p.n_kv_heads) - h0);
+  for (int u = threadIdx.x >> 6; u < units; u += kThreads / 64) {
+    const int h = h0 + (u >> 1);
+    if (u & 1) block_v<DP>(p, v + 2 * h * p.head_dim, at + lay.v + h * lay.tile, scales + p.n_kv_heads + h, a, e);
+    else block_k<DP, MODE>(p, k + 2 * h * p.head_dim, at + h * lay.tile, scales + h, a, e, cs);
   }
 }
 
@@ -319,7 +377,7 @@ hipError_t launch_kv_append(const KvAppendParams& p, int dtype, int n_cus, hipSt
   if (p.total_tokens <= 0 || (!p.q && !p.k)) return hipSuccess;
   const int half = p.rope.half;
   // a workgroup's tokens share their angles' start-up; few tokens are spread over the chip
-  const int tokens_per_wg = p.total_tokens >= 16 * n_cus ? 4 : 1;
+  const int tokens_per_wg = p.total_tokens >= 16 * n_cus ? kMostTokens : 1;
   const unsigned row_wgs = (unsigned)((p.total_tokens + tokens_per_wg - 1) / tokens_per_wg);
   if (dtype != CALVO_E4M3) {
     const size_t lds = (size_t)tokens_per_wg * half * sizeof(attn::f32x2);
@@ -327,14 +385,26 @@ hipError_t launch_kv_append(const KvAppendParams& p, int dtype, int n_cus, hipSt
     else hipLaunchKernelGGL(append_kernel<uint16_t>, dim3(row_wgs), dim3(kThreads), lds, stream, p, tokens_per_wg);
     return hipGetLastError();
   }
-  const int heads_per_wg = 4;
+  // a wave for each K and V of a head where blocks are few; else a block's angles are made once for eight heads
+  const int heads_per_wg = (int64_t)p.n_touched * p.n_kv_heads <= 8 * n_cus ? 2 : 8;
   const int groups = (p.n_kv_heads + heads_per_wg - 1) / heads_per_wg;
   const int kv_wgs = p.k ? p.n_touched * groups : 0;
   const unsigned grid = (unsigned)kv_wgs + (p.q ? row_wgs : 0);
   const size_t lds = (size_t)kBlockTokens * half * sizeof(attn::f32x2);
-  if (p.head_dim <= 64) hipLaunchKernelGGL(append_e4m3_kernel<64>, dim3(grid), dim3(kThreads), lds, stream, p, kv_wgs, heads_per_wg, tokens_per_wg);
-  else if (p.head_dim <= 128) hipLaunchKernelGGL(append_e4m3_kernel<128>, dim3(grid), dim3(kThreads), lds, stream, p, kv_wgs, heads_per_wg, tokens_per_wg);
-  else hipLaunchKernelGGL(append_e4m3_kernel<256>, dim3(grid), dim3(kThreads), lds, stream, p, kv_wgs, heads_per_wg, tokens_per_wg);
+  const int mode = p.rope.rot == 0 ? kNone : p.rope.rot % 8 ? kAnywhere : p.rope.interleaved ? kNeighbours : p.rope.half % 8 ? kAnywhere : kHalves;
+  auto with_mode = [&](auto dp, auto m) {
+    hipLaunchKernelGGL((append_e4m3_kernel<decltype(dp)::value, decltype(m)::value>), dim3(grid), dim3(kThreads), lds, stream, p, kv_wgs, heads_per_wg,
+                       tokens_per_wg);
+  };
+  auto with_width = [&](auto dp) {
+    if (mode == kNone) with_mode(dp, attn::Tag<kNone>{});
+    else if (mode == kHalves) with_mode(dp, attn::Tag<kHalves>{});
+    else if (mode == kNeighbours) with_mode(dp, attn::Tag<kNeighbours>{});
+    else with_mode(dp, attn::Tag<kAnywhere>{});
+  };
+  if (p.head_dim <= 64) with_width(attn::Tag<64>{});
+  else if (p.head_dim <= 128) with_width(attn::Tag<128>{});
+  else with_width(attn::Tag<256>{});
   return hipGetLastError();
 }
 
