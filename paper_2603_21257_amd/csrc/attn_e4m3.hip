@@ -345,8 +345,15 @@ __global__ void __launch_bounds__(64 * C::NW) attn_e4m3_kernel(WinParams p) {
     }
     __syncthreads();
     if (*(const int32_t*)smem != n_splits - 1) return;
+    // every piece's partial result on its way at once where there are few, else 32 of them: a round of loads through the caches takes 1.5 us
     const int here = (int)min(RT, n_rows - row0);
-    for (int row = wave; row < here; row += NW) rows::merge_row<uint16_t, DP, C::ROWS, true>(p, wi.first_item, n_splits, kv, row, row0 + row, wi.q_off);
+    auto merge = [&](auto batch) {
+      for (int row = wave; row < here; row += NW)
+        rows::merge_row<uint16_t, DP, C::ROWS, true, decltype(batch)::value>(p, wi.first_item, n_splits, kv, row, row0 + row, wi.q_off);
+    };
+    if (n_splits <= 8) merge(Tag<8>{});
+    else if (n_splits <= 16 || DP > 128) merge(Tag<16>{});
+    else merge(Tag<32>{});
   }
 }
 

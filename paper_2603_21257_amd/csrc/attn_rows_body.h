@@ -109,7 +109,8 @@ __device__ inline f32x2 load_through(const float* a) {
 
 // One row of a cut tile, one wave: its n pieces from work item `first` on.  SAME: they come from this launch, and no load of theirs stands in a condition
 // (32Q/4KV, D = 128, 20000+1 tokens in four requests 19.6 / 18.8 us a call).
-template <typename T, int DP, int ROWS, bool SAME, typename P>
+// BATCH: pieces asked for at a time.
+template <typename T, int DP, int ROWS, bool SAME, int BATCH = 0, typename P>
 __device__ inline void merge_row(const P& p, int first, int n, int kv, int row, unsigned rho, int q_off) {
   constexpr bool WIN = std::is_same<P, WinParams>::value;
   constexpr int W = DP / 64;                                   // consecutive floats of a lane
@@ -127,7 +128,7 @@ __device__ inline void merge_row(const P& p, int first, int n, int kv, int row, 
     if constexpr (SAME) mine = load_through((const float*)(ml + lane * step));
     else mine = ml[lane * step];
   }
-  constexpr int B = W > 2 ? 8 : 16 / W;                        // loads in flight: the first are on their way while the weights are found
+  constexpr int B = BATCH ? BATCH : W > 2 ? 8 : 16 / W;        // loads in flight: the first are on their way while the weights are found
   vec v[B];
   // Past the end nothing, or the last piece again where that costs no more than the branch: 4 bytes a lane, or one wave of a CU
   auto fetch = [&](int c0) {

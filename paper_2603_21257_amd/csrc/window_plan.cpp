@@ -116,11 +116,15 @@ void choose_pipelined(const WindowShape& s, const std::vector<WindowLens>& lens,
   if (s.force_variant || rows_us >= 0.6 * duo.cost.span) best = std::move(larger ? pipe : duo);
 }
 
-// Packed rows over an 8-bit pool: a step is 64 keys, a workgroup has four waves and two of them fit a CU.
-RowsShape e4m3_shape(int head_dim, bool large) {
-  const int step = head_dim <= 64 ? 6 : head_dim <= 128 ? 10 : 18;
-  if (large && head_dim <= 128) return {32, step + step / 2, 60, 1};
-  return {kFewRows, step, 60, 1};
+// Packed rows over an 8-bit pool, in the units of attn_rows_shape: a step is 64 keys, a workgroup has four waves.  A step of single tokens is the latency of
+// its reads (1.3 us while they leave the memory's rate alone), and the last piece of a tile to arrive merges them in 1.7 us a round of 32.  us a call of
+// one caller, 32Q/8KV, D = 128, with launches of half, one and two workgroups to a CU in mind: 8 requests of 500 to 20000 behind 4096 17.8 / 13.1 / 13.8,
+// four of 4096 12.9 / 10.5 / 12.0, 32 of 300 to 33000 138.7 / 112.3 / 109.9, 60000+1 28.1 / 25.2 / 25.2, 24 of 3000 40.4 / 37.1 / 40.4.
+constexpr int kMostMerged = 32;
+RowsShape e4m3_shape(int head_dim, bool few, bool large) {
+  const int step = head_dim <= 64 ? 8 : head_dim <= 128 ? 13 : 24;
+  if (few) return {kFewRows, step, 20, 1};
+  return large ? RowsShape{32, step + step / 2, 60, 1} : RowsShape{kFewRows, step, 60, 1};
 }
 
 // The launch of the chosen candidate; a packed-rows workgroup merges at most merge_rows rows along (plan_window)
@@ -159,13 +163,17 @@ void plan_window_e4m3(const WindowShape& s, const std::vector<WindowLens>& lens,
     if (large && (few || s.head_dim > 128 || s.force_tile == 1)) break;
     Candidate c;
     c.unit = kE4m3Keys;
-    c.shape = e4m3_shape(s.head_dim, large);
-    c.params = rows_plan_params(c.shape, s.n_kv_heads, 2 * s.n_cus, s.force_splits);
+    c.shape = e4m3_shape(s.head_dim, few, large);
+    c.params = rows_plan_params(c.shape, s.n_kv_heads, few || s.head_dim > 128 ? s.n_cus : 2 * s.n_cus, s.force_splits);
     make_tiles(c, lens, group, window, n_first);
     c.want = plan_pieces(c.tiles, c.params, kMostSlots / c.shape.slots, &c.cost);
+    if (few && !s.force_splits) c.want = std::min(c.want, kMostMerged);
     if (best.tiles.empty() || (large && s.force_tile == 2) || c.cost.span < best.cost.span) best = std::move(c);
   }
-  if (s.head_dim == 128 && s.force_variant != 5 && !few) choose_pipelined(s, lens, window, n_first, 3. + 0.12 * best.cost.span, best);
+  // Where the replays' lengths differ by 2.4 (packed rows in tenths of a microsecond, the pipelined kernels in steps) the two take the same time.  us a call of
+  // one caller, 32Q/8KV, packed rows / kAttnDuo, and that quotient: 4096+64 behind 1024 10.1 / 25.0 (2.4), 1000+100 10.5 / 26.1 (2.3), 60000+5 36.2 / 41.4
+  // (2.1), 0+500 16.7 / 15.6 (2.4), 20000+8 28.7 / 22.5 (2.4), 20000+16 35.2 / 23.5 (2.7), 20000+64 44.2 / 35.7 (3.9), 4096+256 44.8 / 34.3 (3.7).
+  if (s.head_dim == 128 && s.force_variant != 5 && !few) choose_pipelined(s, lens, window, n_first, 0.248 * best.cost.span, best);
   make_plan(s, lens, window, n_first, best, 4, out);
 }
 
