@@ -17,12 +17,15 @@ struct Cfg {
   static constexpr int DB = DP / 16;                           // blocks of 16 d
   static constexpr int ROWS = 16 * QB;
   static constexpr int UNITS = QB * DB;
+  // Steps whose K and V are on their way.  Two where two waves to a SIMD leave registers for it and a wave has many steps (us a call of one caller, one / two:
+  // D = 64, 32Q/8KV 16384+2048 tokens 415 / 391, 8192+512 57.3 / 55.0); not for single tokens, whose waves have one to three (4096+1 behind 1024 7.6 / 8.1)
+  static constexpr int AHEAD = QB_ == 2 && DP_ == 64 ? 2 : 1;
   static constexpr int LDS_O = NW * UNITS * 64 * 16;           // all waves' accumulators
   static constexpr int LDS_BYTES = LDS_O + NW * ROWS * 8;
 };
 
 template <class C>
-__global__ void __launch_bounds__(64 * C::NW) attn_e4m3_kernel(WinParams p) {
+__global__ void __launch_bounds__(64 * C::NW, C::DP > 128 ? 1 : 2) attn_e4m3_kernel(WinParams p) {
   constexpr int DP = C::DP, QB = C::QB, NW = C::NW, KJ = C::KJ, DB = C::DB;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = threadIdx.x & 63;
@@ -70,7 +73,7 @@ __global__ void __launch_bounds__(64 * C::NW) attn_e4m3_kernel(WinParams p) {
   const int32_t* table = p.tables + wi.table_off;
   const int last_blk = (ctx_len + kBlockTokens - 1) / kBlockTokens - 1;
   auto step_at = [&](int st) { return st < wi.first_subs ? st : st + wi.gap; };
-  auto hidden = [&](int key, int pos) { return key > pos || (key <= pos - p.window && key >= p.n_first); };
+  auto hidden = [&](int key, int pos) { return (key > pos) | ((key <= pos - p.window) & (key >= p.n_first)); };
   bool k_ok[KJ];
 #pragma unroll
   for (int j = 0; j < KJ; j++) k_ok[j] = C::FULL || 64 * j + 16 * g < D;
@@ -78,32 +81,34 @@ __global__ void __launch_bounds__(64 * C::NW) attn_e4m3_kernel(WinParams p) {
   const int n_db = D / 16;
 
   int slot_k = 0, slot_v = 0;                                  // of the step that is asked for next
-  u32x4 kx[4][KJ], vx[DB];
-  float ks, vs;
+  constexpr int AHEAD = C::AHEAD;
+  u32x4 kx[AHEAD][4][KJ], vx[AHEAD][DB];
+  float ks[AHEAD], vs[AHEAD];
   const unsigned char* v_next = pool;
   auto look_up = [&](int st) {
     const int b = 4 * step_at(st);
     slot_k = table[min(b + (c >> 2), last_blk)];
     slot_v = table[min(b + g, last_blk)];
   };
-  auto load_k = [&] {
+  auto load_k = [&](auto at) __attribute__((always_inline)) {
+    constexpr int A = decltype(at)::value;
     const unsigned char* kp = pool + (uint64_t)(unsigned)slot_k * lay.bytes;
     v_next = pool + (uint64_t)(unsigned)slot_v * lay.bytes;
-    ks = *(const float*)(kp + lay.scales + 4 * kv);
+    ks[A] = *(const float*)(kp + lay.scales + 4 * kv);
     kp += k_lane;
 #pragma unroll
     for (int kb = 0; kb < 4; kb++)
 #pragma unroll
-      for (int j = 0; j < KJ; j++) kx[kb][j] = *(const u32x4*)(kp + 4 * kb * D + (k_ok[j] ? 64 * j + 16 * g : 0));
+      for (int j = 0; j < KJ; j++) kx[A][kb][j] = *(const u32x4*)(kp + 4 * kb * D + (k_ok[j] ? 64 * j + 16 * g : 0));
   };
-  auto load_v = [&] {
-    vs = *(const float*)(v_next + lay.scales + 4 * (Hkv + kv));
+  auto load_v = [&](auto at) __attribute__((always_inline)) {
+    constexpr int A = decltype(at)::value;
+    vs[A] = *(const float*)(v_next + lay.scales + 4 * (Hkv + kv));
 #pragma unroll
-    for (int db = 0; db < DB; db++) vx[db] = *(const u32x4*)(v_next + v_lane + 256 * (C::FULL ? db : min(db, n_db - 1)));
+    for (int db = 0; db < DB; db++) vx[A][db] = *(const u32x4*)(v_next + v_lane + 256 * (C::FULL ? db : min(db, n_db - 1)));
   };
 
   const int st_begin = wi.sub_begin + wave;
-  int st = st_begin;
   const int st_end = min(wi.sub_end, pos_max / 64 + 1 - wi.gap);
   bf16x8 qx[QB][2 * KJ];
   const f32x4 zero4 = {0.f, 0.f, 0.f, 0.f};
@@ -118,22 +123,16 @@ __global__ void __launch_bounds__(64 * C::NW) attn_e4m3_kernel(WinParams p) {
   }
   const float c2 = p.scale * 1.4426950408889634f;
 
-  // NaN in V where some row may not see it: the product would take weight 0 times it and gets zeros instead; the rows that do see it are told below.
-  bool dirty = false;
-  auto set_apart = [&]() __attribute__((always_inline)) {
-    dirty = true;
-    const bool none = not_finite(vs);
-#pragma unroll
-    for (int db = 0; db < DB; db++)
-#pragma unroll
-      for (int i = 0; i < 4; i++) vx[db][i] = none ? 0u : vx[db][i] & ~((nan_bytes(vx[db][i]) >> 7) * 0xffu);
-    if (none) vs = 1.f;
-  };
+  unsigned dirty = 0;
+  // Steps that every row sees in full spend nothing on masks: in front of them are those with first tokens and those that windows begin in
+  const int st_full = (pos_min + 1) / 64 - wi.gap, full_from = max(wi.first_subs, (pos_max - p.window < 0 ? 0 : (pos_max - p.window) / 64 + 1) - wi.gap);
 
-  // One step.  DIAG: some row does not see all of its keys.  MORE: the wave has another one, which this one asks for.
-  auto step = [&](auto diag_tag, auto more_tag) __attribute__((always_inline)) {
-    constexpr bool DIAG = decltype(diag_tag)::value != 0, MORE = decltype(more_tag)::value != 0;
+  // Step st, whose K and V are in registers A.  MORE: the wave has a step AHEAD further on, which this one asks for.
+  auto step = [&](int st, auto at, auto more_tag) __attribute__((always_inline)) {
+    constexpr int A = decltype(at)::value;
+    constexpr bool MORE = decltype(more_tag)::value != 0;
     const int k0 = step_at(st) * 64;
+    const bool hides = st < full_from || st >= st_full;        // some row does not see all of the keys
     f32x4 s[4][QB];
 #pragma unroll
     for (int kb = 0; kb < 4; kb++)
@@ -142,19 +141,21 @@ __global__ void __launch_bounds__(64 * C::NW) attn_e4m3_kernel(WinParams p) {
 #pragma unroll
     for (int j = 0; j < KJ; j++)
 #pragma unroll
-      for (int h = 0; h < 2; h++)
+      for (int h = 0; h < 2; h++) {
 #pragma unroll
         for (int kb = 0; kb < 4; kb++) {
-          const u32x4 x = kx[kb][j];
-          const bf16x8 a = widen(C::FULL || k_ok[j] ? x[2 * h] : 0u, C::FULL || k_ok[j] ? x[2 * h + 1] : 0u, ks);
+          const u32x4 x = kx[A][kb][j];
+          const bf16x8 a = widen(C::FULL || k_ok[j] ? x[2 * h] : 0u, C::FULL || k_ok[j] ? x[2 * h + 1] : 0u, ks[A]);
 #pragma unroll
           for (int qb = 0; qb < QB; qb++) s[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qx[qb][2 * j + h], s[kb][qb], 0, 0, 0);
         }
+        __builtin_amdgcn_sched_barrier(0);                     // four operands at a time in bf16: more would cost the second wave of a SIMD
+      }
     if constexpr (MORE) {
-      load_k();
-      look_up(st + 2 * NW);                                    // clamped to the last block
+      load_k(at);
+      look_up(st + (AHEAD + 1) * NW);                          // clamped to the last block
     }
-    if constexpr (DIAG) {
+    if (hides) {
 #pragma unroll
       for (int kb = 0; kb < 4; kb++)
 #pragma unroll
@@ -196,27 +197,28 @@ __global__ void __launch_bounds__(64 * C::NW) attn_e4m3_kernel(WinParams p) {
 #pragma unroll
         for (int db = 0; db < DB; db++) o[qb][db] *= alpha[qb];
     }
-    if constexpr (DIAG) {
-      unsigned bad = not_finite(vs) ? 1u : 0u;
+    if (hides) {                                               // NaN in V: the product takes weight 0 times it, also for rows that do not see the key
+      dirty |= not_finite(vs[A]) ? 1u : 0u;
 #pragma unroll
       for (int db = 0; db < DB; db++)
 #pragma unroll
-        for (int i = 0; i < 4; i++) bad |= nan_bytes(vx[db][i]);
-      if (__builtin_expect(__builtin_amdgcn_ballot_w64(bad != 0) != 0, 0)) set_apart();
+        for (int i = 0; i < 4; i++) dirty |= nan_bytes(vx[A][db][i]);
     }
 #pragma unroll
     for (int h = 0; h < 2; h++)
 #pragma unroll
       for (int db = 0; db < DB; db++) {
-        const bf16x8 a = widen(vx[db][2 * h], vx[db][2 * h + 1], vs);
+        const bf16x8 a = widen(vx[A][db][2 * h], vx[A][db][2 * h + 1], vs[A]);
 #pragma unroll
         for (int qb = 0; qb < QB; qb++) o[qb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pw[qb][h], o[qb][db], 0, 0, 0);
+        if (db % 4 == 3) __builtin_amdgcn_sched_barrier(0);
       }
-    if constexpr (MORE) load_v();
+    if constexpr (MORE) load_v(at);
   };
 
-  if (st < st_end) {
-    look_up(st);
+  const int n_steps = st_begin < st_end ? (st_end - st_begin + NW - 1) / NW : 0;
+  if (n_steps > 0) {
+    look_up(st_begin);
 #pragma unroll
     for (int qb = 0; qb < QB; qb++)
 #pragma unroll
@@ -225,46 +227,105 @@ __global__ void __launch_bounds__(64 * C::NW) attn_e4m3_kernel(WinParams p) {
         for (int h = 0; h < 2; h++)
           qx[qb][2 * j + h] = *(const bf16x8*)((const unsigned char*)p.q + (qrow[qb] * D + (k_ok[j] ? 64 * j + 16 * g + 8 * h : 0)) * 2);
     __builtin_amdgcn_sched_barrier(0);
-    load_k();
-    look_up(st + NW);
+    load_k(Tag<0>{});
+    look_up(st_begin + NW);
     __builtin_amdgcn_sched_barrier(0);
-    load_v();
+    load_v(Tag<0>{});
     __builtin_amdgcn_sched_barrier(0);
+    auto settle_q = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int qb = 0; qb < QB; qb++)
+      for (int qb = 0; qb < QB; qb++)
 #pragma unroll
-      for (int i = 0; i < 2 * KJ; i++) {
-        if (!C::FULL && !k_ok[i / 2]) qx[qb][i] = __builtin_bit_cast(bf16x8, (u32x4){0u, 0u, 0u, 0u});
-        asm volatile("" : "+v"(qx[qb][i]));
+        for (int i = 0; i < 2 * KJ; i++) {
+          if (!C::FULL && !k_ok[i / 2]) qx[qb][i] = __builtin_bit_cast(bf16x8, (u32x4){0u, 0u, 0u, 0u});
+          asm volatile("" : "+v"(qx[qb][i]));
+        }
+    };
+    // No request of a step stands in a condition, and none is for a step that the wave does not have
+    int st = st_begin, left = n_steps;
+    if constexpr (AHEAD == 1) {
+      settle_q();
+      for (; left > 1; left--, st += NW) step(st, Tag<0>{}, Tag<1>{});
+      step(st, Tag<0>{}, Tag<0>{});
+    } else {
+      // a single step asks for the context's last block beside its own: a path without it would cost half as many registers again
+      load_k(Tag<1>{});
+      look_up(st + 2 * NW);
+      __builtin_amdgcn_sched_barrier(0);
+      load_v(Tag<1>{});
+      __builtin_amdgcn_sched_barrier(0);
+      settle_q();
+      // an odd number of steps asks for the last one again at the end
+      for (; left > 2; left -= 2, st += 2 * NW) {
+        step(st, Tag<0>{}, Tag<1>{});
+        step(st + NW, Tag<1>{}, Tag<1>{});
       }
-    // Steps that every row sees in full spend nothing on masks: in front of them those with first tokens and those that windows begin in
-    const int st_last = st_end - NW, st_full = min(st_last, (pos_min + 1) / 64 - wi.gap);
-    const int begin = pos_max - p.window < 0 ? 0 : (pos_max - p.window) / 64 + 1;
-    const int full_from = min(st_last, max(wi.first_subs, begin - wi.gap));
-    for (; st < full_from; st += NW) step(Tag<1>{}, Tag<1>{});
-    for (; st < st_full; st += NW) step(Tag<0>{}, Tag<1>{});
-    for (; st < st_last; st += NW) step(Tag<1>{}, Tag<1>{});
-    step(Tag<1>{}, Tag<0>{});
+      step(st, Tag<0>{}, Tag<0>{});
+      if (left == 2) step(st + NW, Tag<1>{}, Tag<0>{});
+    }
   }
-  // The wave's keys again, one by one, for the V that was set apart: what a row sees of it makes that element of its sum NaN.
-  if (__builtin_expect(dirty, 0)) {
+  // With such V the wave's rows meet its keys again, 16 at a time and V key by key: a row adds weight times V of the keys that it sees and touches no
+  // other.  Rare, so it is written for few registers.
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(dirty != 0) != 0, 0)) {
+    static_for<0, QB>([&](auto qb_tag) __attribute__((always_inline)) {
+      constexpr int qb = decltype(qb_tag)::value;
+#pragma unroll
+      for (int db = 0; db < DB; db++) o[qb][db] = zero4;
+      m[qb] = -INFINITY;
+      l[qb] = 0.f;
 #pragma unroll 1
-    for (int s0 = st_begin; s0 < st_end; s0 += NW)
+      for (int b4 = 0; b4 < 4 * n_steps; b4++) {
+        const int key0 = 64 * step_at(st_begin + NW * (b4 >> 2)) + kBlockTokens * (b4 & 3), rest = min(kBlockTokens, ctx_len - key0);
+        if (rest <= 0) break;
+        const unsigned char* blk = pool + (uint64_t)(unsigned)table[key0 / kBlockTokens] * lay.bytes;
+        const float k_scale = *(const float*)(blk + lay.scales + 4 * kv), v_scale = *(const float*)(blk + lay.scales + 4 * (Hkv + kv));
+        const unsigned char* kr = blk + (unsigned)kv * lay.tile + min(c, rest - 1) * D;
+        f32x4 x = zero4;
 #pragma unroll 1
-      for (int key = 64 * step_at(s0); key < min(64 * step_at(s0) + 64, ctx_len); key++) {
-        const unsigned char* blk = pool + (uint64_t)(unsigned)table[key / kBlockTokens] * lay.bytes;
-        const bool all = not_finite(*(const float*)(blk + lay.scales + 4 * (Hkv + kv)));
-        const unsigned char* v = blk + lay.v + (unsigned)kv * lay.tile + key % kBlockTokens;
+        for (int j = 0; j < KJ; j++)
 #pragma unroll
-        for (int db = 0; db < DB; db++)
-#pragma unroll
-          for (int r = 0; r < 4; r++) {
-            const bool bad = all || (v[16 * min(16 * db + 4 * g + r, D - 1)] & 0x7f) == 0x7f;
-#pragma unroll
-            for (int qb = 0; qb < QB; qb++)
-              if (bad && !hidden(key, posq[qb])) o[qb][db][r] = __builtin_nanf("");
+          for (int h = 0; h < 2; h++) {
+            const int d = 64 * j + 16 * g + 8 * h;
+            u32x2 y = {0u, 0u};
+            u32x4 q = {0u, 0u, 0u, 0u};
+            if (C::FULL || d < D) {
+              y = *(const u32x2*)(kr + d);
+              q = *(const u32x4*)((const unsigned char*)p.q + (qrow[qb] * D + d) * 2);
+            }
+            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(y[0], y[1], k_scale), __builtin_bit_cast(bf16x8, q), x, 0, 0, 0);
           }
+        float mx = -INFINITY, w[4];
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+          if (hidden(key0 + 4 * g + r, posq[qb])) x[r] = -INFINITY;
+          mx = fmaxf(mx, x[r]);
+        }
+        const float mn = fmaxf(m[qb], quad_max(mx) * c2), ref = mn == -INFINITY ? 0.f : mn, a = __builtin_amdgcn_exp2f(m[qb] - ref);
+        m[qb] = mn;
+        l[qb] *= a;
+#pragma unroll
+        for (int db = 0; db < DB; db++) o[qb][db] *= a;
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+          w[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c2, -ref));
+          l[qb] += w[r];
+        }
+#pragma unroll 1
+        for (int t = 0; t < rest; t++) {
+          const float mine = t & 2 ? (t & 1 ? w[3] : w[2]) : (t & 1 ? w[1] : w[0]);
+          const float wk = __shfl(mine, 16 * (t >> 2) + c);
+          const bool sees = !hidden(key0 + t, posq[qb]);
+          const unsigned char* v = blk + lay.v + (unsigned)kv * lay.tile + t;
+#pragma unroll
+          for (int db = 0; db < DB; db++)
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+              const bf16x2 y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[16 * min(16 * db + 4 * g + r, D - 1)], v_scale, false);
+              if (sees) o[qb][db][r] = __builtin_fmaf(wk, (float)y[0], o[qb][db][r]);
+            }
+        }
       }
+    });
   }
 
   // ---- row sums over the four lanes of a row, then over the waves
