@@ -177,13 +177,17 @@ struct RopeParams {
   int32_t rot, half;         // rotated elements of a head; half of them
   int32_t interleaved;
 };
+// A block that takes new tokens: those at its places [places & 255, places >> 8) are the batch's from `token` on, the first at position `pos` of its request
+struct TouchedBlock {
+  int32_t slot, token, pos, places;
+};
 struct KvAppendParams {
   const void *q, *k, *v;     // q, or k and v, may be NULL
   void* q_out;
   int64_t q_row, k_row, v_row;   // bytes from one token's row to the next
   unsigned char* pool_layer;
   const ReqDesc* reqs;
-  const int32_t* touched;    // CALVO_E4M3: blocks that the requests in front of one write, [n_reqs + 1]
+  const TouchedBlock* touched;   // CALVO_E4M3
   const int32_t* tables;
   int32_t n_reqs, total_tokens, n_touched;
   int32_t n_q_heads, n_kv_heads, head_dim;

@@ -279,8 +279,10 @@ int window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, i
   w->mass_at = pad4(w->arrived_at + n_arrived);
   w->add_at = w->mass_at + n_mass * kMass;
   w->append_at = w->add_at + w->mass.adds.size() * kAdd;
-  w->touched_at = w->append_at + (size_t)n_reqs * kApp;
-  w->tables_at = w->touched_at + (e4m3 ? (size_t)n_reqs + 1 : 0);
+  w->touched_at = pad4(w->append_at + (size_t)n_reqs * kApp);
+  for (int r = 0; r < n_reqs && e4m3; r++)
+    if (reqs[r].n_new) w->n_touched += (int)(blocks_of((int64_t)reqs[r].n_cached + reqs[r].n_new) - reqs[r].n_cached / kBlockTokens);
+  w->tables_at = w->touched_at + (size_t)w->n_touched * (sizeof(TouchedBlock) / 4);
   w->offs_at = pad4(w->tables_at + (size_t)table_words);
   auto offs_of = [](int64_t n_tab) { return n_tab + kTablePad + (n_tab & 1); };
   size_t n_offs = 0;
@@ -296,6 +298,7 @@ int window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, i
   int32_t* h = w->buf.h;
   std::vector<int32_t> table_off((size_t)n_reqs), mass_table((size_t)n_reqs), q_off((size_t)n_reqs);
   int64_t* offs = (int64_t*)(h + w->offs_at);
+  TouchedBlock* touched = (TouchedBlock*)(h + w->touched_at);
   size_t at = 0, offs_at = 0;
   int32_t q = 0;
   for (int r = 0; r < n_reqs; r++) {
@@ -314,12 +317,14 @@ int window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, i
     h[w->tables_at + at + n_tab] = n_tab ? reqs[r].block_table[n_tab - 1] : 0;
     const ReqDesc a = {(int32_t)at, reqs[r].n_cached, reqs[r].n_new, q};
     memcpy(h + w->append_at + (size_t)r * kApp, &a, sizeof a);
-    if (e4m3) h[w->touched_at + (size_t)r] = w->n_touched;
-    if (reqs[r].n_new) w->n_touched += (int)((int64_t)n_tab - reqs[r].n_cached / kBlockTokens);
+    for (size_t b = (size_t)reqs[r].n_cached / kBlockTokens; e4m3 && reqs[r].n_new && b < n_tab; b++) {
+      const int32_t from = std::max(reqs[r].n_cached, (int32_t)b * kBlockTokens), to = (int32_t)std::min<int64_t>(tokens, (int64_t)(b + 1) * kBlockTokens);
+      const int32_t first = (int32_t)b * kBlockTokens;
+      *touched++ = {reqs[r].block_table[b], q + from - reqs[r].n_cached, from, (from - first) | (to - first) << 8};
+    }
     at += n_tab + 1;
     q += reqs[r].n_new;
   }
-  if (e4m3) h[w->touched_at + (size_t)n_reqs] = w->n_touched;
   for (size_t i = 0; i < n_items; i++) {
     const WindowPiece& x = w->plan.items[i];
     const WinItem d = {x.tile, x.sub_begin, x.sub_end, x.n_splits, x.first_item, table_off[x.req], reqs[x.req].n_cached, reqs[x.req].n_new,
@@ -351,8 +356,9 @@ int queue_append(calvo_window* w, KvAppendParams& p, unsigned char* pool_layer) 
   calvo_ctx* c = w->c;
   const calvo_config& cf = c->cfg;
   const int32_t* d = w->buf.d;
+  if (((int64_t)w->n_touched * ((cf.n_kv_heads + 1) / 2) + w->total) * 256 > kMostThreads) return fail(CALVO_EINVAL, "too many new tokens");
   p.pool_layer = pool_layer;
-  p.reqs = (const ReqDesc*)(d + w->append_at); p.touched = d + w->touched_at; p.tables = d + w->tables_at;
+  p.reqs = (const ReqDesc*)(d + w->append_at); p.touched = (const TouchedBlock*)(d + w->touched_at); p.tables = d + w->tables_at;
   p.n_reqs = w->n_reqs; p.total_tokens = w->total; p.n_touched = w->n_touched;
   p.n_q_heads = cf.n_q_heads; p.n_kv_heads = cf.n_kv_heads; p.head_dim = cf.head_dim;
   HIP_TRY(launch_kv_append(p, cf.dtype, c->n_cus, c->s_compute));
@@ -402,7 +408,6 @@ int kv_append(calvo_window* w, int layer, const void* k_new, int64_t k_stride, c
     for (const Range& a : to)
       for (const Range& b : from)
         if ((rc = apart(a, b)) != CALVO_OK) return rc;
-    if (((int64_t)w->n_touched * ((cf.n_kv_heads + 1) / 2) + w->total) * 256 > kMostThreads) return fail(CALVO_EINVAL, "too many new tokens");
   }
   ON_DEVICE(c);
   if ((rc = queue_behind_layer(c, layer)) != CALVO_OK) return rc;

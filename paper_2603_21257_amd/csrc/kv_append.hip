@@ -62,8 +62,9 @@ struct Chunk<float> {
   static __device__ u32x4 packed(const float (&x)[4]) { return (u32x4){bits_of(x[0]), bits_of(x[1]), bits_of(x[2]), bits_of(x[3])}; }
 };
 
-// How pairs lie in 16-byte chunks of a row: none is rotated, a pair's elements are in the same places of two chunks, in one chunk, or anywhere
-enum { kNone, kHalves, kNeighbours, kAnywhere };
+// How pairs lie in the 16-byte chunks that the lanes of a block have: none is rotated, a pair's elements are in the same places of two chunks, those two
+// belong to one lane, in one chunk, or anywhere
+enum { kNone, kHalves, kWhole, kNeighbours, kAnywhere };
 
 // Chunk ch of a head's row, rotated.  cs: (cos, sin) of the token's pairs.
 template <typename T>
@@ -191,153 +192,170 @@ __device__ inline float number(const u32x4& v, int k) { return float_of(k & 1 ? 
 // K or V of one (block, head) for a wave.  Tokens [a, e) of the block are new, those in front of a stay (at the larger scale), those behind e become
 // zeros.  What the block holds is asked for first: it is there when the new values' scale is known.
 template <int DP, int MODE>
-__device__ inline void block_k(const KvAppendParams& p, const unsigned char* src, unsigned char* tile, float* scale, int a, int e, const f32x2* cs) {
-  constexpr int NC = DP / 64;                                  // pairs of 8-element chunks that a lane has
-  const int lane = threadIdx.x & 63, t = lane >> 2, D = p.head_dim, rot = p.rope.rot, half = p.rope.half;
-  const bool is_new = t >= a && t < e;
-  const unsigned char* row = src + (t - a) * p.k_row;
-  const f32x2* my_cs = cs + (t - a) * half;
-  const float old_scale = a > 0 ? *scale : 0.f;
+struct BlockK {
+  static constexpr int NC = DP / 64;                           // pairs of 8-element chunks that a lane has
   u32x4 y[NC], own[NC][2], other[NC][2];
-  float x[NC][2][8];
-  // all that is asked for, then chunk by chunk: many at a time would need the registers of two waves
+  float old_scale;
+
+  __device__ void ask(const KvAppendParams& p, const unsigned char* src, const unsigned char* tile, const float* scale, int a, int e) {
+    const int lane = threadIdx.x & 63, t = lane >> 2, D = p.head_dim, rot = p.rope.rot, half = p.rope.half;
+    const unsigned char* row = src + (t - a) * p.k_row;
+    old_scale = a > 0 ? *scale : 0.f;
 #pragma unroll
-  for (int i = 0; i < NC; i++) {
-    const int d = 64 * i + 16 * (lane & 3);
-    y[i] = (u32x4){0u, 0u, 0u, 0u};
-    if (t < a && d < D) y[i] = *(const u32x4*)(tile + t * D + d);
-#pragma unroll
-    for (int h = 0; h < 2; h++) {
-      const int d0 = d + 8 * h;
-      own[i][h] = other[i][h] = (u32x4){0u, 0u, 0u, 0u};
-      if (is_new && d < D) {
-        own[i][h] = *(const u32x4*)(row + 2 * d0);
-        if (MODE == kHalves && d0 < rot) other[i][h] = *(const u32x4*)(row + 2 * (d0 < half ? d0 + half : d0 - half));
-      }
-    }
-  }
-  __builtin_amdgcn_sched_barrier(0);
-  unsigned top = 0;
-#pragma unroll
-  for (int i = 0; i < NC; i++)
-#pragma unroll
-    for (int h = 0; h < 2; h++) {
-      const int d0 = 64 * i + 16 * (lane & 3) + 8 * h;
-#pragma unroll
-      for (int k = 0; k < 8; k++) x[i][h][k] = number(own[i][h], k);
-      if (MODE != kNone && is_new && d0 < rot) {
-        const bool lower = d0 < half;
-        if constexpr (MODE == kHalves) {
-          const f32x2* c2 = my_cs + (lower ? d0 : d0 - half);
-#pragma unroll
-          for (int k = 0; k < 8; k++) {
-            const float o = number(other[i][h], k);
-            x[i][h][k] = x[i][h][k] * c2[k][0] + (lower ? -o : o) * c2[k][1];
-          }
-        } else if constexpr (MODE == kNeighbours) {
-#pragma unroll
-          for (int k = 0; k < 8; k += 2) {
-            const f32x2 c = my_cs[(d0 + k) >> 1];
-            const float u = x[i][h][k], v = x[i][h][k + 1];
-            x[i][h][k] = u * c[0] - v * c[1];
-            x[i][h][k + 1] = v * c[0] + u * c[1];
-          }
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; k++) {
-            const int d = d0 + k;
-            if (d >= rot) continue;
-            const bool first = p.rope.interleaved ? d % 2 == 0 : d < half;
-            const int i2 = p.rope.interleaved ? d / 2 : first ? d : d - half, d2 = p.rope.interleaved ? d ^ 1 : first ? d + half : d - half;
-            const f32x2 c = my_cs[i2];
-            const float o = Chunk<uint16_t>::one(row, d2);
-            x[i][h][k] = x[i][h][k] * c[0] + (first ? -o : o) * c[1];
-            __builtin_amdgcn_sched_barrier(0);
-          }
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < 8; k++) top = max(top, bits_of(x[i][h][k]) & 0x7fffffffu);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  const int before = (int)(bits_of(old_scale) >> 23) & 255, ex = max(scale_exponent(wave_max(top)), before);
-#pragma unroll
-  for (int i = 0; i < NC; i++) {
-    const int d = 64 * i + 16 * (lane & 3);
-    if (is_new) {
+    for (int i = 0; i < NC; i++) {
+      const int d = 64 * i + 16 * (lane & 3);
+      y[i] = (u32x4){0u, 0u, 0u, 0u};
+      if (t < a && d < D) y[i] = *(const u32x4*)(tile + t * D + d);
 #pragma unroll
       for (int h = 0; h < 2; h++) {
-        float v[8];
-#pragma unroll
-        for (int k = 0; k < 8; k++) v[k] = __builtin_amdgcn_ldexpf(x[i][h][k], 127 - ex);
-        y[i][2 * h] = e4m3::pack4(v[0], v[1], v[2], v[3]);
-        y[i][2 * h + 1] = e4m3::pack4(v[4], v[5], v[6], v[7]);
+        const int d0 = d + 8 * h;
+        own[i][h] = other[i][h] = (u32x4){0u, 0u, 0u, 0u};
+        if (t >= a && t < e && d < D) {
+          own[i][h] = *(const u32x4*)(row + 2 * d0);
+          if (MODE == kHalves && d0 < rot) other[i][h] = *(const u32x4*)(row + 2 * (d0 < half ? d0 + half : d0 - half));
+        }
       }
-    } else if (t < a && ex != before) {
-#pragma unroll
-      for (int k = 0; k < 4; k++) y[i][k] = rescaled(y[i][k], ex - before);
     }
-    if (ex == 255) y[i] = (u32x4){0u, 0u, 0u, 0u};
-    if (d < D) *(u32x4*)(tile + t * D + d) = y[i];
   }
-  if (lane == 0) *scale = scale_of(ex);
-}
+
+  __device__ void store(const KvAppendParams& p, const unsigned char* src, unsigned char* tile, float* scale, int a, int e, const f32x2* cs) {
+    const int lane = threadIdx.x & 63, t = lane >> 2, D = p.head_dim, rot = p.rope.rot, half = p.rope.half;
+    const bool is_new = t >= a && t < e;
+    const unsigned char* row = src + (t - a) * p.k_row;
+    const f32x2* my_cs = cs + (t - a) * half;
+    float x[NC][2][8];
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < NC; i++)
+#pragma unroll
+      for (int h = 0; h < 2; h++) {
+        const int d0 = 64 * i + 16 * (lane & 3) + 8 * h;
+#pragma unroll
+        for (int k = 0; k < 8; k++) x[i][h][k] = number(own[i][h], k);
+        if (MODE != kNone && is_new && d0 < rot) {
+          const bool lower = d0 < half;
+          if constexpr (MODE == kHalves || MODE == kWhole) {
+            const f32x2* c2 = my_cs + (lower ? d0 : d0 - half);
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+              const float o = number(MODE == kWhole ? own[(i + NC / 2) % NC][h] : other[i][h], k);
+              x[i][h][k] = x[i][h][k] * c2[k][0] + (lower ? -o : o) * c2[k][1];
+            }
+          } else if constexpr (MODE == kNeighbours) {
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+              const f32x2 c = my_cs[(d0 + k) >> 1];
+              const float u = x[i][h][k], v = x[i][h][k + 1];
+              x[i][h][k] = u * c[0] - v * c[1];
+              x[i][h][k + 1] = v * c[0] + u * c[1];
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+              const int d = d0 + k;
+              if (d >= rot) continue;
+              const bool first = p.rope.interleaved ? d % 2 == 0 : d < half;
+              const int i2 = p.rope.interleaved ? d / 2 : first ? d : d - half, d2 = p.rope.interleaved ? d ^ 1 : first ? d + half : d - half;
+              const f32x2 c = my_cs[i2];
+              const float o = Chunk<uint16_t>::one(row, d2);
+              x[i][h][k] = x[i][h][k] * c[0] + (first ? -o : o) * c[1];
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; k++) top = max(top, bits_of(x[i][h][k]) & 0x7fffffffu);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    const int before = (int)(bits_of(old_scale) >> 23) & 255, ex = max(scale_exponent(wave_max(top)), before);
+#pragma unroll
+    for (int i = 0; i < NC; i++) {
+      const int d = 64 * i + 16 * (lane & 3);
+      if (is_new) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+          float v[8];
+#pragma unroll
+          for (int k = 0; k < 8; k++) v[k] = __builtin_amdgcn_ldexpf(x[i][h][k], 127 - ex);
+          y[i][2 * h] = e4m3::pack4(v[0], v[1], v[2], v[3]);
+          y[i][2 * h + 1] = e4m3::pack4(v[4], v[5], v[6], v[7]);
+        }
+      } else if (t < a && ex != before) {
+#pragma unroll
+        for (int k = 0; k < 4; k++) y[i][k] = rescaled(y[i][k], ex - before);
+      }
+      if (ex == 255) y[i] = (u32x4){0u, 0u, 0u, 0u};
+      if (d < D) *(u32x4*)(tile + t * D + d) = y[i];
+    }
+    if (lane == 0) *scale = scale_of(ex);
+  }
+};
 
 template <int DP>
-__device__ inline void block_v(const KvAppendParams& p, const unsigned char* src, unsigned char* tile, float* scale, int a, int e) {
-  constexpr int ND = (DP + 127) / 128;                         // pairs of neighbouring d that a lane has
-  const int lane = threadIdx.x & 63, D = p.head_dim;
-  const float old_scale = a > 0 ? *scale : 0.f;
+struct BlockV {
+  static constexpr int ND = (DP + 127) / 128;                  // pairs of neighbouring d that a lane has
   u32x4 old[ND][2];
   unsigned x[ND][16];
+  float old_scale;
+
+  __device__ void ask(const KvAppendParams& p, const unsigned char* src, const unsigned char* tile, const float* scale, int a, int e) {
+    const int lane = threadIdx.x & 63, D = p.head_dim;
+    old_scale = a > 0 ? *scale : 0.f;
 #pragma unroll
-  for (int i = 0; i < ND; i++)
-#pragma unroll
-    for (int h = 0; h < 2; h++) {
+    for (int i = 0; i < ND; i++) {
       const int d = 128 * i + 2 * lane;
-      old[i][h] = (u32x4){0u, 0u, 0u, 0u};
-      if (a > 0 && d < D) old[i][h] = *(const u32x4*)(tile + 16 * (d + h));
-    }
 #pragma unroll
-  for (int i = 0; i < ND; i++)
-#pragma unroll
-    for (int t = 0; t < 16; t++) {
-      const int d = 128 * i + 2 * lane;
-      x[i][t] = t >= a && t < e && d < D ? *(const unsigned*)(src + (t - a) * p.v_row + 2 * d) : 0u;
-    }
-  unsigned top = 0;
-#pragma unroll
-  for (int i = 0; i < ND; i++)
-#pragma unroll
-    for (int t = 0; t < 16; t++) top = max(max(top, x[i][t] & 0x7fff0000u), x[i][t] << 16 & 0x7fff0000u);
-  const int before = (int)(bits_of(old_scale) >> 23) & 255, ex = max(scale_exponent(wave_max(top)), before);
-#pragma unroll
-  for (int i = 0; i < ND; i++) {
-    const int d = 128 * i + 2 * lane;
-    if (d >= D) continue;
-#pragma unroll
-    for (int h = 0; h < 2; h++) {
-      u32x4 y;
-#pragma unroll
-      for (int k = 0; k < 4; k++) {
-        float v[4];
-#pragma unroll
-        for (int j = 0; j < 4; j++) v[j] = __builtin_amdgcn_ldexpf(float_of(h ? x[i][4 * k + j] & 0xffff0000u : x[i][4 * k + j] << 16), 127 - ex);
-        const int n_old = min(max(a - 4 * k, 0), 4);           // of these four
-        unsigned was = old[i][h][k];
-        if (ex != before && n_old) was = rescaled(was, ex - before);
-        const unsigned keep = n_old == 4 ? 0xffffffffu : (1u << 8 * n_old) - 1;
-        y[k] = ex == 255 ? 0u : (was & keep) | (e4m3::pack4(v[0], v[1], v[2], v[3]) & ~keep);
+      for (int h = 0; h < 2; h++) {
+        old[i][h] = (u32x4){0u, 0u, 0u, 0u};
+        if (a > 0 && d < D) old[i][h] = *(const u32x4*)(tile + 16 * (d + h));
       }
-      *(u32x4*)(tile + 16 * (d + h)) = y;
+#pragma unroll
+      for (int t = 0; t < 16; t++) x[i][t] = t >= a && t < e && d < D ? *(const unsigned*)(src + (t - a) * p.v_row + 2 * d) : 0u;
     }
   }
-  if (lane == 0) *scale = scale_of(ex);
+
+  __device__ void store(const KvAppendParams& p, unsigned char* tile, float* scale, int a) {
+    const int lane = threadIdx.x & 63, D = p.head_dim;
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < ND; i++)
+#pragma unroll
+      for (int t = 0; t < 16; t++) top = max(max(top, x[i][t] & 0x7fff0000u), x[i][t] << 16 & 0x7fff0000u);
+    const int before = (int)(bits_of(old_scale) >> 23) & 255, ex = max(scale_exponent(wave_max(top)), before);
+#pragma unroll
+    for (int i = 0; i < ND; i++) {
+      const int d = 128 * i + 2 * lane;
+      if (d >= D) continue;
+#pragma unroll
+      for (int h = 0; h < 2; h++) {
+        u32x4 y;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+          float v[4];
+#pragma unroll
+          for (int j = 0; j < 4; j++) v[j] = __builtin_amdgcn_ldexpf(float_of(h ? x[i][4 * k + j] & 0xffff0000u : x[i][4 * k + j] << 16), 127 - ex);
+          const int n_old = min(max(a - 4 * k, 0), 4);           // of these four
+          unsigned was = old[i][h][k];
+          if (ex != before && n_old) was = rescaled(was, ex - before);
+          const unsigned keep = n_old == 4 ? 0xffffffffu : (1u << 8 * n_old) - 1;
+          y[k] = ex == 255 ? 0u : (was & keep) | (e4m3::pack4(v[0], v[1], v[2], v[3]) & ~keep);
+        }
+        *(u32x4*)(tile + 16 * (d + h)) = y;
+      }
+    }
+    if (lane == 0) *scale = scale_of(ex);
+  }
+};
+
+// as many as leave every instantiation its registers
+constexpr int waves_per_simd(int dp, int mode) {
+  if (dp > 128) return mode == kHalves || mode == kAnywhere ? 1 : 2;
+  return mode == kAnywhere ? 2 : mode == kHalves && dp > 64 ? 3 : 4;
 }
 
 // The workgroups of the first kv_wgs take a touched block and heads_per_wg heads each, a wave K or V of a head at a time; the others rows of q.
 template <int DP, int MODE>
-__global__ void __launch_bounds__(kThreads, (DP > 128 ? 2 : 4) / (MODE == kAnywhere ? 2 : 1)) append_e4m3_kernel(KvAppendParams p, int kv_wgs, int heads_per_wg, int tokens_per_wg) {
+__global__ void __launch_bounds__(kThreads, waves_per_simd(DP, MODE)) append_e4m3_kernel(KvAppendParams p, int kv_wgs, int heads_per_wg, int tokens_per_wg) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   f32x2* const cs = (f32x2*)smem;
   if ((int)blockIdx.x >= kv_wgs) {
@@ -346,27 +364,41 @@ __global__ void __launch_bounds__(kThreads, (DP > 128 ? 2 : 4) / (MODE == kAnywh
     return;
   }
   const int groups = (p.n_kv_heads + heads_per_wg - 1) / heads_per_wg;
-  const int blk = blockIdx.x / groups, h0 = (blockIdx.x % groups) * heads_per_wg;
-  const int r = last_at_or_below(p.n_reqs, blk, [&](int i) { return p.touched[i]; });
-  const ReqDesc rd = p.reqs[r];
-  const int b = rd.prefix_len / kBlockTokens + blk - p.touched[r];
-  const int first = max(rd.prefix_len, kBlockTokens * b), a = first - kBlockTokens * b;
-  const int e = min(kBlockTokens, rd.prefix_len + rd.suffix_len - kBlockTokens * b);
-  const int tok = rd.q_off + first - rd.prefix_len, half = p.rope.half;
+  const int h0 = (blockIdx.x % groups) * heads_per_wg;
+  const const_i32p item = (const_i32p)(uintptr_t)(p.touched + blockIdx.x / groups);
+  const int slot = item[0], tok = item[1], first = item[2], a = item[3] & 255, e = item[3] >> 8;
   const E4m3Block lay = e4m3_block(p.n_kv_heads, p.head_dim);
-  unsigned char* const at = p.pool_layer + (uint64_t)(unsigned)p.tables[rd.table_off + b] * lay.bytes;
-  for (int i = threadIdx.x; MODE != kNone && i < (e - a) * half; i += kThreads) {
-    const int t = i / half;
-    cs[i] = cos_sin(p.rope, p.rope.positions ? p.rope.positions[tok + t] : first + t, i - t * half);
-  }
-  __syncthreads();
+  unsigned char* const at = p.pool_layer + (uint64_t)(unsigned)slot * lay.bytes;
   float* const scales = (float*)(at + lay.scales);
   const unsigned char *k = (const unsigned char*)p.k + tok * p.k_row, *v = (const unsigned char*)p.v + tok * p.v_row;
-  const int units = 2 * (min(h0 + heads_per_wg, p.n_kv_heads) - h0);
-  for (int u = threadIdx.x >> 6; u < units; u += kThreads / 64) {
-    const int h = h0 + (u >> 1);
-    if (u & 1) block_v<DP>(p, v + 2 * h * p.head_dim, at + lay.v + h * lay.tile, scales + p.n_kv_heads + h, a, e);
-    else block_k<DP, MODE>(p, k + 2 * h * p.head_dim, at + h * lay.tile, scales + h, a, e, cs);
+  // unit u: K (u even) or V of head h0 + u / 2; a wave has units of one kind.  The next one's values are on their way while one is stored, the first
+  // one's while the angles are made.
+  const int units = 2 * (min(h0 + heads_per_wg, p.n_kv_heads) - h0), u0 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = p.rope.half;
+  auto angles = [&] {
+    for (int i = threadIdx.x; MODE != kNone && i < (e - a) * half; i += kThreads) {
+      const int t = i / half;
+      cs[i] = cos_sin(p.rope, p.rope.positions ? p.rope.positions[tok + t] : first + t, i - t * half);
+    }
+    __syncthreads();
+  };
+  auto all_units = [&](auto&& here, auto&& next, auto&& ask, auto&& store) {
+    if (u0 < units) ask(here, h0 + (u0 >> 1));
+    angles();
+    for (int u = u0; u < units; u += kThreads / 64) {
+      const bool more = u + kThreads / 64 < units;
+      if (more) ask(next, h0 + (u >> 1) + kThreads / 128);
+      store(here, h0 + (u >> 1));
+      if (more) here = next;
+    }
+  };
+  if (u0 & 1) {
+    BlockV<DP> here, next;
+    all_units(here, next, [&](auto& x, int h) { x.ask(p, v + 2 * h * p.head_dim, at + lay.v + h * lay.tile, scales + p.n_kv_heads + h, a, e); },
+              [&](auto& x, int h) { x.store(p, at + lay.v + h * lay.tile, scales + p.n_kv_heads + h, a); });
+  } else {
+    BlockK<DP, MODE> here, next;
+    all_units(here, next, [&](auto& x, int h) { x.ask(p, k + 2 * h * p.head_dim, at + h * lay.tile, scales + h, a, e); },
+              [&](auto& x, int h) { x.store(p, k + 2 * h * p.head_dim, at + h * lay.tile, scales + h, a, e, cs); });
   }
 }
 
@@ -391,7 +423,7 @@ hipError_t launch_kv_append(const KvAppendParams& p, int dtype, int n_cus, hipSt
   const int kv_wgs = p.k ? p.n_touched * groups : 0;
   const unsigned grid = (unsigned)kv_wgs + (p.q ? row_wgs : 0);
   const size_t lds = (size_t)kBlockTokens * half * sizeof(attn::f32x2);
-  const int mode = p.rope.rot == 0 ? kNone : p.rope.rot % 8 ? kAnywhere : p.rope.interleaved ? kNeighbours : p.rope.half % 8 ? kAnywhere : kHalves;
+  const int mode = p.rope.rot == 0 ? kNone : p.rope.rot % 8 ? kAnywhere : p.rope.interleaved ? kNeighbours : p.rope.half % 8 ? kAnywhere : p.rope.rot == p.head_dim && (p.rope.rot == 128 || p.rope.rot == 256) ? kWhole : kHalves;
   auto with_mode = [&](auto dp, auto m) {
     hipLaunchKernelGGL((append_e4m3_kernel<decltype(dp)::value, decltype(m)::value>), dim3(grid), dim3(kThreads), lds, stream, p, kv_wgs, heads_per_wg,
                        tokens_per_wg);
@@ -399,6 +431,7 @@ hipError_t launch_kv_append(const KvAppendParams& p, int dtype, int n_cus, hipSt
   auto with_width = [&](auto dp) {
     if (mode == kNone) with_mode(dp, attn::Tag<kNone>{});
     else if (mode == kHalves) with_mode(dp, attn::Tag<kHalves>{});
+    else if (mode == kWhole) with_mode(dp, attn::Tag<kWhole>{});
     else if (mode == kNeighbours) with_mode(dp, attn::Tag<kNeighbours>{});
     else with_mode(dp, attn::Tag<kAnywhere>{});
   };
