@@ -153,6 +153,12 @@ __global__ void __launch_bounds__(kThreads) append_kernel(KvAppendParams p, int 
   move_rows<T, true>(p, t0, min(tokens_per_wg, p.total_tokens - t0), (f32x2*)smem);
 }
 
+__global__ void __launch_bounds__(kThreads) append_q_kernel(KvAppendParams p, int tokens_per_wg) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int t0 = blockIdx.x * tokens_per_wg;
+  move_rows<uint16_t, false>(p, t0, min(tokens_per_wg, p.total_tokens - t0), (f32x2*)smem);
+}
+
 // ---- pools of 8-bit floats
 
 // Biased exponent of the scale for values of at most `top` (its bits; more than those of an infinity: NaN): the smallest 2^e with top <= 448 2^e = 1.75 * 2^(e + 8)
@@ -421,7 +427,10 @@ hipError_t launch_kv_append(const KvAppendParams& p, int dtype, int n_cus, hipSt
   const int heads_per_wg = (int64_t)p.n_touched * p.n_kv_heads <= 8 * n_cus ? 2 : 8;
   const int groups = (p.n_kv_heads + heads_per_wg - 1) / heads_per_wg;
   const int kv_wgs = p.k ? p.n_touched * groups : 0;
-  const unsigned grid = (unsigned)kv_wgs + (p.q ? row_wgs : 0);
+  // Many rows of q go by themselves: beside the blocks they would have half the waves to a CU
+  const bool apart = p.q && kv_wgs && tokens_per_wg > 1;
+  if (apart) hipLaunchKernelGGL(append_q_kernel, dim3(row_wgs), dim3(kThreads), (size_t)tokens_per_wg * half * sizeof(attn::f32x2), stream, p, tokens_per_wg);
+  const unsigned grid = (unsigned)kv_wgs + (p.q && !apart ? row_wgs : 0);
   const size_t lds = (size_t)kBlockTokens * half * sizeof(attn::f32x2);
   const int mode = p.rope.rot == 0 ? kNone : p.rope.rot % 8 ? kAnywhere : p.rope.interleaved ? kNeighbours : p.rope.half % 8 ? kAnywhere : p.rope.rot == p.head_dim && (p.rope.rot == 128 || p.rope.rot == 256) ? kWhole : kHalves;
   auto with_mode = [&](auto dp, auto m) {
