@@ -32,8 +32,8 @@
  * CALVO_E4M3: a block (in the pool and in host KV) is
  *    K [Hkv][B][D] bytes, V [Hkv][D][B] bytes, scales fp32 [K, V][Hkv], and room up to a multiple of 128 bytes (calvo_block_bytes)
  * A byte is an 8-bit float of the OCP format E4M3 (four bits of exponent, three of fraction, largest 448, no infinity, 0x7f and 0xff NaN) and
- * stands for its value times the scale of its K or V, block and head.  A scale is a power of two, 2^-126 to 2^119: only its exponent is looked at;
- * one that is not finite makes all its values NaN.  Loading moves such blocks as any others, at half the bytes of bf16; calvo_window_prepare,
+ * stands for its value times the scale of its K or V, block and head.  A scale is a power of two, 2^-126 to 2^120: only its exponent is looked at;
+ * one that is not finite makes all its values NaN.  What a byte stands for is read as bf16 would hold it: below 2^-126 it may be zero, from 2^128 on it is infinite.  Loading moves such blocks as any others, at half the bytes of bf16; calvo_window_prepare,
  * calvo_kv_append, calvo_window_attn and the calls without a pool take them, the others refuse with CALVO_EINVAL.
  * The paper names blocks, tiers and the context/query split but no block size,
  * layout or precision; these are this library's definitions.

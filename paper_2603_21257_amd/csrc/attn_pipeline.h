@@ -120,7 +120,7 @@ struct WinPipeCfg : PipeCfg<NW_, RING_, HB_> {
 };
 // Over a pool of 8-bit floats (attn_e4m3_pipe.hip, kv_e4m3.h).  Widening two numbers takes the vector ALU 8 cycles, as much as an exponential, and every wave needs
 // all of K and V: they are widened once for the workgroup, on their way from the pool through registers into LDS, not behind every wave's LDS read (sixteen
-// instructions a step and wave instead of 64: 0+16384 tokens 1721 / E8_US us a call).  Step t asks for 16 bytes a lane of K(t + KA) and V(t + VA) and their
+// instructions a step and wave instead of 64: 0+16384 tokens 1721 / 1672 us a call).  Step t asks for 16 bytes a lane of K(t + KA) and V(t + VA) and their
 // blocks' scales, and stores K(t + KA - 2) and V(t + VA - 2), asked for two steps before.
 // V lies d-major in the pool and in LDS: a lane's eight keys of an operand are 16 bytes in a row if the k-slot order is slot 8g + 4kb + r <-> key
 // 8g + 4kb + r, so row 4g + r of score tile kb is that key here.  K's chunks are swizzled by the lane that reads the row, V's by d / 4.

@@ -27,8 +27,8 @@ using namespace attn;
 __device__ inline unsigned bits_of(float x) { return __builtin_bit_cast(unsigned, x); }
 __device__ inline float float_of(unsigned x) { return __builtin_bit_cast(float, x); }
 
-// Eight bytes times 2^(exponent of s), exact in bf16: four significant bits, and the scales that an append chooses keep them inside bf16's range.
-// An exponent of ones makes NaN of every byte.
+// Eight bytes times 2^(exponent of s), exact in bf16, whose eight significant bits hold four, but for values below its normal range or beyond its
+// largest.  An exponent of ones makes NaN of every byte.
 __device__ inline bf16x8 widen(unsigned a, unsigned b, float s) {
   const unsigned x[4] = {__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, false)),
                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, true)),
