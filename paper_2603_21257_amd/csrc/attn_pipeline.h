@@ -123,7 +123,7 @@ struct WinPipeCfg : PipeCfg<NW_, RING_, HB_> {
 // instructions a step and wave instead of 64: 0+16384 tokens 1721 / 1672 us a call).  Step t asks for 16 bytes a lane of K(t + KA) and V(t + VA) and their
 // blocks' scales, and stores K(t + KA - 2) and V(t + VA - 2), asked for two steps before.
 // V lies d-major in the pool and in LDS: a lane's eight keys of an operand are 16 bytes in a row if the k-slot order is slot 8g + 4kb + r <-> key
-// 8g + 4kb + r, so row 4g + r of score tile kb is that key here.  K's chunks are swizzled by the lane that reads the row, V's by d / 4.
+// 8g + 4kb + r, so row 4g + r of score tile kb is that key here.  K's chunks are swizzled by the lane that reads the row, V's by d / 4 (v_swizzle).
 template <int NW_, int RING_, int HB_>
 struct WinPipe8Cfg : WinPipeCfg<NW_, RING_, HB_> {
   static_assert(NW_ == 4, "a wave takes a quarter of a sub-tile's 4 KiB");
@@ -131,6 +131,10 @@ struct WinPipe8Cfg : WinPipeCfg<NW_, RING_, HB_> {
   static constexpr int VA = 4;                         // the drain's V is stored by the last steady step
   static constexpr bool E8 = true;
 };
+// 0, 2, 3, 1.  A 16-byte LDS read serves, at a time, rows c / 4 = 0 and 3 of one g and 1 and 2 of the next, or the other way round: with row r's chunks at
+// g ^ r those share banks, with these they do not: 32 conflict cycles less a step and wave, of 64 (the stores count the others; 28096+28, 28304+61 and
+// 38304+209 tokens, 32Q/8KV, 171 / 170 us a call).
+__device__ inline int v_swizzle(int r) { return 0x78 >> 2 * r & 3; }
 // WIN: the reference of a row that has seen no key.  Finite, so that the weight of a hidden key (score -inf) is 0 against it; far enough below
 // every score for the first visible one to pass the bound.
 constexpr float kNoRef = -3e38f;
@@ -303,7 +307,7 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
 #pragma unroll
     for (int h = 0; h < 2; h++) {
       put_k[h] = smem + row * kRow + (((2 * (lane & 7) + h) ^ ((row & 3) | (row >> 3) << 2)) << 4);
-      put_v[h] = smem + kVBase + d * 64 + (((2 * wblk + h) ^ (d >> 2 & 3)) << 4);
+      put_v[h] = smem + kVBase + d * 64 + (((2 * wblk + h) ^ v_swizzle(d >> 2 & 3)) << 4);
     }
   }
   auto ask_k = [&](const unsigned char* base, u32x4& x, float& s) {
@@ -405,7 +409,7 @@ __device__ __forceinline__ void attn_pipeline(const typename Cfg_::Params& p, un
   const lds_u8* va_addr[8];
 #pragma unroll
   for (int db = 0; db < 8; db++)
-    va_addr[db] = E8 ? lds + kVBase + 1024 * db + 64 * c + ((g ^ (c >> 2)) << 4)
+    va_addr[db] = E8 ? lds + kVBase + 1024 * db + 64 * c + ((g ^ v_swizzle(c >> 2)) << 4)
                      : lds + kVBase + v_row * kRow + ((2 * (db ^ (v_row & 7)) + ((c & 3) >> 1)) << 4) + (c & 1) * 8;
   auto v_opnd = [&](const lds_u8* a) -> bf16x8 {
     if constexpr (E8) return read_k(a);
