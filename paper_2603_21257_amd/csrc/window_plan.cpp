@@ -124,7 +124,10 @@ constexpr int kMostMerged = 32;
 RowsShape e4m3_shape(int head_dim, bool few, bool large) {
   const int step = head_dim <= 64 ? 8 : head_dim <= 128 ? 13 : 24;
   if (few) return {kFewRows, step, 20, 1};
-  return large ? RowsShape{32, step + step / 2, 60, 1} : RowsShape{kFewRows, step, 60, 1};
+  // Wider heads are cut earlier (60 / 45, D = 256: 700+60 tokens, 8Q/2KV 13.5 / 12.0, 500+33, 4Q/4KV 12.1 / 11.4, nine other shapes the same); with 45
+  // 128-wide ones would stay on packed rows too rarely (4096+64 behind 1024, 32Q/8KV 10.0 / 14.7)
+  const int start = head_dim > 128 ? 45 : 60;
+  return large ? RowsShape{32, step + step / 2, start, 1} : RowsShape{kFewRows, step, start, 1};
 }
 
 // The launch of the chosen candidate; a packed-rows workgroup merges at most merge_rows rows along (plan_window)
