@@ -36,76 +36,99 @@ __device__ inline f32x2 cos_sin(const RopeParams& rope, int pos, int i) {
   return (f32x2){c, s};
 }
 
+// Where pair i of a token is in LDS, and pairs from one token to the next.  Lanes that read at once have four chunks of a row 128 bytes apart and some tokens:
+// rows of whole bank sets would put all of these on one bank (8000 tokens into an 8-bit pool, 32Q/8KV, D = 128: the blocks' launch 20.7 / 12.8 us).  An
+// element more for every 32 and rows of 2 mod 4 elements spread them.
+__host__ __device__ inline int angle_at(int i) { return i + (i >> 5); }
+__host__ __device__ inline int angle_row(int half) { return (half + (half >> 5) + 1) / 4 * 4 + 2; }
+
+// Where element d's partner is, of pairs (i, i + half); an element that is not rotated is its own
+__device__ inline int partner(const RopeParams& rope, int d) { return d < rope.half ? d + rope.half : d < rope.rot ? d - rope.half : d; }
+
 // 16 bytes of a head's row as numbers, and back
 template <typename T>
 struct Chunk;
 template <>
 struct Chunk<uint16_t> {
   static constexpr int N = 8;
-  static __device__ void read(const unsigned char* a, float (&x)[8]) {
-    const u32x4 v = *(const u32x4*)a;
+  static __device__ float number(const u32x4& v, int k) { return float_of(k & 1 ? v[k >> 1] & 0xffff0000u : v[k >> 1] << 16); }
+  // the partners of chunk elements d0 ...; two at a time where halves are even
+  static __device__ u32x4 partners(const RopeParams& rope, const unsigned char* row, int d0) {
+    u32x4 y;
+    const unsigned short* x = (const unsigned short*)row;
+    if (rope.half % 2 == 0) {
 #pragma unroll
-    for (int i = 0; i < 8; i++) x[i] = float_of(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16);
+      for (int i = 0; i < 4; i++) y[i] = *(const unsigned*)(x + partner(rope, d0 + 2 * i));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; i++) y[i] = x[partner(rope, d0 + 2 * i)] | (unsigned)x[partner(rope, d0 + 2 * i + 1)] << 16;
+    }
+    return y;
   }
-  static __device__ float one(const unsigned char* row, int d) { return float_of((unsigned)((const unsigned short*)row)[d] << 16); }
   static __device__ u32x4 packed(const float (&x)[8]) { return (u32x4){pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])}; }
 };
 template <>
 struct Chunk<float> {
   static constexpr int N = 4;
-  static __device__ void read(const unsigned char* a, float (&x)[4]) {
-    const f32x4 v = *(const f32x4*)a;
+  static __device__ float number(const u32x4& v, int k) { return float_of(v[k]); }
+  static __device__ u32x4 partners(const RopeParams& rope, const unsigned char* row, int d0) {
+    u32x4 y;
 #pragma unroll
-    for (int i = 0; i < 4; i++) x[i] = v[i];
+    for (int i = 0; i < 4; i++) y[i] = ((const unsigned*)row)[partner(rope, d0 + i)];
+    return y;
   }
-  static __device__ float one(const unsigned char* row, int d) { return ((const float*)row)[d]; }
   static __device__ u32x4 packed(const float (&x)[4]) { return (u32x4){bits_of(x[0]), bits_of(x[1]), bits_of(x[2]), bits_of(x[3])}; }
 };
 
-// How pairs lie in the 16-byte chunks that the lanes of a block have: none is rotated, a pair's elements are in the same places of two chunks, those two
-// belong to one lane, in one chunk, or anywhere
+// How pairs lie in 16-byte chunks: none is rotated, a pair's elements are in the same places of two chunks, those two belong to one lane (of a block in 8 bits),
+// they are neighbours, or anywhere
 enum { kNone, kHalves, kWhole, kNeighbours, kAnywhere };
 
-// Chunk ch of a head's row, rotated.  cs: (cos, sin) of the token's pairs.
-template <typename T>
+// Chunk ch of a head's row, rotated.  cs: (cos, sin) of the token's pairs.  Both elements of its pairs are asked for before either is waited for.
+template <typename T, int MODE>
 __device__ inline void rotated(const RopeParams& rope, const unsigned char* row, int ch, const f32x2* cs, float (&x)[Chunk<T>::N]) {
   constexpr int N = Chunk<T>::N;
   const int d0 = ch * N;
-  Chunk<T>::read(row + 16 * ch, x);
-  if (d0 >= rope.rot) return;
-  if (rope.interleaved) {
+  const bool lower = d0 < rope.half;
+  const u32x4 own = *(const u32x4*)(row + 16 * ch);
+  u32x4 other = own;
+  if (MODE == kHalves && d0 < rope.rot) other = *(const u32x4*)(row + 16 * ch + (lower ? rope.half : -rope.half) * (int)sizeof(T));
+  if (MODE == kAnywhere && d0 < rope.rot) other = Chunk<T>::partners(rope, row, d0);
+#pragma unroll
+  for (int i = 0; i < N; i++) x[i] = Chunk<T>::number(own, i);
+  if (MODE == kNone || d0 >= rope.rot) return;
+  if constexpr (MODE == kNeighbours) {
+    const f32x2* t = cs + angle_at(d0 >> 1);
 #pragma unroll
     for (int i = 0; i < N; i += 2)
       if (d0 + i < rope.rot) {
-        const f32x2 t = cs[(d0 + i) >> 1];
         const float a = x[i], b = x[i + 1];
-        x[i] = a * t[0] - b * t[1];
-        x[i + 1] = b * t[0] + a * t[1];
+        x[i] = a * t[i >> 1][0] - b * t[i >> 1][1];
+        x[i + 1] = b * t[i >> 1][0] + a * t[i >> 1][1];
       }
-  } else if (rope.half % N == 0) {
-    const bool lower = d0 < rope.half;
-    float y[N];
-    Chunk<T>::read(row + 16 * ch + (lower ? rope.half : -rope.half) * (int)sizeof(T), y);
-    const f32x2* t = cs + (lower ? d0 : d0 - rope.half);
+  } else if constexpr (MODE == kHalves) {
+    const f32x2* t = cs + angle_at(lower ? d0 : d0 - rope.half);
 #pragma unroll
-    for (int i = 0; i < N; i++) x[i] = x[i] * t[i][0] + (lower ? -y[i] : y[i]) * t[i][1];
+    for (int i = 0; i < N; i++) {
+      const float o = Chunk<T>::number(other, i);
+      x[i] = x[i] * t[i][0] + (lower ? -o : o) * t[i][1];
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < N; i++) {
       const int d = d0 + i;
-      if (d >= rope.rot) continue;
-      const bool lower = d < rope.half;
-      const f32x2 t = cs[lower ? d : d - rope.half];
-      const float y = Chunk<T>::one(row, lower ? d + rope.half : d - rope.half);
-      x[i] = x[i] * t[0] + (lower ? -y : y) * t[1];
+      const bool first = d < rope.half;
+      const f32x2 t = cs[angle_at(min(first ? d : d - rope.half, rope.half - 1))];
+      const float o = Chunk<T>::number(other, i);
+      if (d < rope.rot) x[i] = x[i] * t[0] + (first ? -o : o) * t[1];
     }
   }
 }
 
 constexpr int kThreads = 256, kMostTokens = 4;       // of a workgroup: one wave finds the place of each
 
-// Rows of tokens [t0, t0 + n): q -> q_out, and where the pool holds the same type k and v -> pool.  cs: room for n * rot / 2 pairs.
-template <typename T, bool KV>
+// Rows of tokens [t0, t0 + n): q -> q_out, and where the pool holds the same type k and v -> pool.  cs: room for n rows of angles.
+template <typename T, bool KV, int MODE>
 __device__ inline void move_rows(const KvAppendParams& p, int t0, int n, f32x2* cs) {
   constexpr int N = Chunk<T>::N;
   __shared__ int pos_of[kMostTokens];
@@ -121,8 +144,11 @@ __device__ inline void move_rows(const KvAppendParams& p, int t0, int n, f32x2* 
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < n * half; i += kThreads) cs[i] = cos_sin(p.rope, pos_of[i / half], i % half);
-  __syncthreads();
+  const int cs_row = angle_row(half);
+  if constexpr (MODE != kNone) {
+    for (int i = threadIdx.x; i < n * half; i += kThreads) cs[i / half * cs_row + angle_at(i % half)] = cos_sin(p.rope, pos_of[i / half], i % half);
+    __syncthreads();
+  }
   const int chunks = p.head_dim / N, row_chunks = p.n_kv_heads * chunks;
   const int nq = p.q ? p.n_q_heads * chunks : 0, nk = KV && p.k ? row_chunks : 0;
   const int all = nq + 2 * nk;
@@ -130,14 +156,14 @@ __device__ inline void move_rows(const KvAppendParams& p, int t0, int n, f32x2* 
     const int t = i / all, j = i - t * all, tok = t0 + t;
     if (j < nq) {
       float x[N];
-      rotated<T>(p.rope, (const unsigned char*)p.q + tok * p.q_row + (j / chunks) * p.head_dim * (int)sizeof(T), j % chunks, cs + t * half, x);
+      rotated<T, MODE>(p.rope, (const unsigned char*)p.q + tok * p.q_row + (j / chunks) * p.head_dim * (int)sizeof(T), j % chunks, cs + t * cs_row, x);
       ((u32x4*)p.q_out)[(int64_t)tok * nq + j] = Chunk<T>::packed(x);
     } else if constexpr (KV) {
       const int k = j - nq;
       u32x4* dst = (u32x4*)p.pool_layer + row_of[t] * row_chunks;
       if (k < nk) {
         float x[N];
-        rotated<T>(p.rope, (const unsigned char*)p.k + tok * p.k_row + (k / chunks) * p.head_dim * (int)sizeof(T), k % chunks, cs + t * half, x);
+        rotated<T, MODE>(p.rope, (const unsigned char*)p.k + tok * p.k_row + (k / chunks) * p.head_dim * (int)sizeof(T), k % chunks, cs + t * cs_row, x);
         dst[k] = Chunk<T>::packed(x);
       } else {
         dst[kBlockTokens * row_chunks + k - nk] = *(const u32x4*)((const unsigned char*)p.v + tok * p.v_row + 16 * (k - nk));
@@ -146,17 +172,18 @@ __device__ inline void move_rows(const KvAppendParams& p, int t0, int n, f32x2* 
   }
 }
 
-template <typename T>
+template <typename T, int MODE>
 __global__ void __launch_bounds__(kThreads) append_kernel(KvAppendParams p, int tokens_per_wg) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int t0 = blockIdx.x * tokens_per_wg;
-  move_rows<T, true>(p, t0, min(tokens_per_wg, p.total_tokens - t0), (f32x2*)smem);
+  move_rows<T, true, MODE>(p, t0, min(tokens_per_wg, p.total_tokens - t0), (f32x2*)smem);
 }
 
+template <int MODE>
 __global__ void __launch_bounds__(kThreads) append_q_kernel(KvAppendParams p, int tokens_per_wg) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int t0 = blockIdx.x * tokens_per_wg;
-  move_rows<uint16_t, false>(p, t0, min(tokens_per_wg, p.total_tokens - t0), (f32x2*)smem);
+  move_rows<uint16_t, false, MODE>(p, t0, min(tokens_per_wg, p.total_tokens - t0), (f32x2*)smem);
 }
 
 // ---- pools of 8-bit floats
@@ -192,8 +219,7 @@ __device__ inline unsigned rescaled(unsigned x, int shift) {
   return e4m3::pack4(v[0], v[1], v[2], v[3]);
 }
 
-// element k of a chunk of bf16
-__device__ inline float number(const u32x4& v, int k) { return float_of(k & 1 ? v[k >> 1] & 0xffff0000u : v[k >> 1] << 16); }
+__device__ inline float number(const u32x4& v, int k) { return Chunk<uint16_t>::number(v, k); }
 
 // K or V of one (block, head) for a wave.  Tokens [a, e) of the block are new, those in front of a stay (at the larger scale), those behind e become
 // zeros.  What the block holds is asked for first: it is there when the new values' scale is known.
@@ -219,16 +245,16 @@ struct BlockK {
         if (t >= a && t < e && d < D) {
           own[i][h] = *(const u32x4*)(row + 2 * d0);
           if (MODE == kHalves && d0 < rot) other[i][h] = *(const u32x4*)(row + 2 * (d0 < half ? d0 + half : d0 - half));
+          if (MODE == kAnywhere && d0 < rot) other[i][h] = Chunk<uint16_t>::partners(p.rope, row, d0);
         }
       }
     }
   }
 
-  __device__ void store(const KvAppendParams& p, const unsigned char* src, unsigned char* tile, float* scale, int a, int e, const f32x2* cs) {
+  __device__ void store(const KvAppendParams& p, unsigned char* tile, float* scale, int a, int e, const f32x2* cs) {
     const int lane = threadIdx.x & 63, t = lane >> 2, D = p.head_dim, rot = p.rope.rot, half = p.rope.half;
     const bool is_new = t >= a && t < e;
-    const unsigned char* row = src + (t - a) * p.k_row;
-    const f32x2* my_cs = cs + (t - a) * half;
+    const f32x2* my_cs = cs + (t - a) * angle_row(half);
     float x[NC][2][8];
     unsigned top = 0;
 #pragma unroll
@@ -241,31 +267,30 @@ struct BlockK {
         if (MODE != kNone && is_new && d0 < rot) {
           const bool lower = d0 < half;
           if constexpr (MODE == kHalves || MODE == kWhole) {
-            const f32x2* c2 = my_cs + (lower ? d0 : d0 - half);
+            const f32x2* c2 = my_cs + angle_at(lower ? d0 : d0 - half);
 #pragma unroll
             for (int k = 0; k < 8; k++) {
               const float o = number(MODE == kWhole ? own[(i + NC / 2) % NC][h] : other[i][h], k);
               x[i][h][k] = x[i][h][k] * c2[k][0] + (lower ? -o : o) * c2[k][1];
             }
           } else if constexpr (MODE == kNeighbours) {
+            const f32x2* c2 = my_cs + angle_at(d0 >> 1);
 #pragma unroll
             for (int k = 0; k < 8; k += 2) {
-              const f32x2 c = my_cs[(d0 + k) >> 1];
               const float u = x[i][h][k], v = x[i][h][k + 1];
-              x[i][h][k] = u * c[0] - v * c[1];
-              x[i][h][k + 1] = v * c[0] + u * c[1];
+              if (d0 + k < rot) {
+                x[i][h][k] = u * c2[k >> 1][0] - v * c2[k >> 1][1];
+                x[i][h][k + 1] = v * c2[k >> 1][0] + u * c2[k >> 1][1];
+              }
             }
           } else {
 #pragma unroll
             for (int k = 0; k < 8; k++) {
               const int d = d0 + k;
-              if (d >= rot) continue;
-              const bool first = p.rope.interleaved ? d % 2 == 0 : d < half;
-              const int i2 = p.rope.interleaved ? d / 2 : first ? d : d - half, d2 = p.rope.interleaved ? d ^ 1 : first ? d + half : d - half;
-              const f32x2 c = my_cs[i2];
-              const float o = Chunk<uint16_t>::one(row, d2);
-              x[i][h][k] = x[i][h][k] * c[0] + (first ? -o : o) * c[1];
-              __builtin_amdgcn_sched_barrier(0);
+              const bool first = d < half;
+              const f32x2 c = my_cs[angle_at(min(first ? d : d - half, half - 1))];
+              const float o = number(other[i][h], k);
+              if (d < rot) x[i][h][k] = x[i][h][k] * c[0] + (first ? -o : o) * c[1];
             }
           }
         }
@@ -366,7 +391,7 @@ __global__ void __launch_bounds__(kThreads, waves_per_simd(DP, MODE)) append_e4m
   f32x2* const cs = (f32x2*)smem;
   if ((int)blockIdx.x >= kv_wgs) {
     const int t0 = ((int)blockIdx.x - kv_wgs) * tokens_per_wg;
-    move_rows<uint16_t, false>(p, t0, min(tokens_per_wg, p.total_tokens - t0), cs);
+    move_rows<uint16_t, false, MODE == kWhole ? (int)kHalves : MODE>(p, t0, min(tokens_per_wg, p.total_tokens - t0), cs);
     return;
   }
   const int groups = (p.n_kv_heads + heads_per_wg - 1) / heads_per_wg;
@@ -382,8 +407,8 @@ __global__ void __launch_bounds__(kThreads, waves_per_simd(DP, MODE)) append_e4m
   const int units = 2 * (min(h0 + heads_per_wg, p.n_kv_heads) - h0), u0 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = p.rope.half;
   auto angles = [&] {
     for (int i = threadIdx.x; MODE != kNone && i < (e - a) * half; i += kThreads) {
-      const int t = i / half;
-      cs[i] = cos_sin(p.rope, p.rope.positions ? p.rope.positions[tok + t] : first + t, i - t * half);
+      const int t = i / half, j = i - t * half;
+      cs[t * angle_row(half) + angle_at(j)] = cos_sin(p.rope, p.rope.positions ? p.rope.positions[tok + t] : first + t, j);
     }
     __syncthreads();
   };
@@ -404,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, waves_per_simd(DP, MODE)) append_e4m
   } else {
     BlockK<DP, MODE> here, next;
     all_units(here, next, [&](auto& x, int h) { x.ask(p, k + 2 * h * p.head_dim, at + h * lay.tile, scales + h, a, e); },
-              [&](auto& x, int h) { x.store(p, k + 2 * h * p.head_dim, at + h * lay.tile, scales + h, a, e, cs); });
+              [&](auto& x, int h) { x.store(p, at + h * lay.tile, scales + h, a, e, cs); });
   }
 }
 
@@ -413,14 +438,24 @@ __global__ void __launch_bounds__(kThreads, waves_per_simd(DP, MODE)) append_e4m
 hipError_t launch_kv_append(const KvAppendParams& p, int dtype, int n_cus, hipStream_t stream) {
   using namespace append;
   if (p.total_tokens <= 0 || (!p.q && !p.k)) return hipSuccess;
-  const int half = p.rope.half;
+  const int half = p.rope.half, per_chunk = dtype == CALVO_F32 ? 4 : 8;
   // a workgroup's tokens share their angles' start-up; few tokens are spread over the chip
   const int tokens_per_wg = p.total_tokens >= 16 * n_cus ? kMostTokens : 1;
   const unsigned row_wgs = (unsigned)((p.total_tokens + tokens_per_wg - 1) / tokens_per_wg);
+  const size_t angles = (size_t)angle_row(half) * sizeof(attn::f32x2);
+  const int mode = p.rope.rot == 0 ? kNone : p.rope.interleaved ? kNeighbours : half % per_chunk ? kAnywhere : kHalves;
+  auto with_mode = [&](auto&& f) {
+    if (mode == kNone) f(attn::Tag<kNone>{});
+    else if (mode == kHalves) f(attn::Tag<kHalves>{});
+    else if (mode == kNeighbours) f(attn::Tag<kNeighbours>{});
+    else f(attn::Tag<kAnywhere>{});
+  };
   if (dtype != CALVO_E4M3) {
-    const size_t lds = (size_t)tokens_per_wg * half * sizeof(attn::f32x2);
-    if (dtype == CALVO_F32) hipLaunchKernelGGL(append_kernel<float>, dim3(row_wgs), dim3(kThreads), lds, stream, p, tokens_per_wg);
-    else hipLaunchKernelGGL(append_kernel<uint16_t>, dim3(row_wgs), dim3(kThreads), lds, stream, p, tokens_per_wg);
+    with_mode([&](auto m) {
+      constexpr int M = decltype(m)::value;
+      if (dtype == CALVO_F32) hipLaunchKernelGGL((append_kernel<float, M>), dim3(row_wgs), dim3(kThreads), tokens_per_wg * angles, stream, p, tokens_per_wg);
+      else hipLaunchKernelGGL((append_kernel<uint16_t, M>), dim3(row_wgs), dim3(kThreads), tokens_per_wg * angles, stream, p, tokens_per_wg);
+    });
     return hipGetLastError();
   }
   // a wave for each K and V of a head where blocks are few; else a block's angles are made once for eight heads
@@ -429,20 +464,18 @@ hipError_t launch_kv_append(const KvAppendParams& p, int dtype, int n_cus, hipSt
   const int kv_wgs = p.k ? p.n_touched * groups : 0;
   // Many rows of q go by themselves: beside the blocks they would have half the waves to a CU
   const bool apart = p.q && kv_wgs && tokens_per_wg > 1;
-  if (apart) hipLaunchKernelGGL(append_q_kernel, dim3(row_wgs), dim3(kThreads), (size_t)tokens_per_wg * half * sizeof(attn::f32x2), stream, p, tokens_per_wg);
+  if (apart)
+    with_mode([&](auto m) {
+      hipLaunchKernelGGL(append_q_kernel<decltype(m)::value>, dim3(row_wgs), dim3(kThreads), tokens_per_wg * angles, stream, p, tokens_per_wg);
+    });
   const unsigned grid = (unsigned)kv_wgs + (p.q && !apart ? row_wgs : 0);
-  const size_t lds = (size_t)kBlockTokens * half * sizeof(attn::f32x2);
-  const int mode = p.rope.rot == 0 ? kNone : p.rope.rot % 8 ? kAnywhere : p.rope.interleaved ? kNeighbours : p.rope.half % 8 ? kAnywhere : p.rope.rot == p.head_dim && (p.rope.rot == 128 || p.rope.rot == 256) ? kWhole : kHalves;
-  auto with_mode = [&](auto dp, auto m) {
-    hipLaunchKernelGGL((append_e4m3_kernel<decltype(dp)::value, decltype(m)::value>), dim3(grid), dim3(kThreads), lds, stream, p, kv_wgs, heads_per_wg,
-                       tokens_per_wg);
+  auto launch = [&](auto dp, auto m) {
+    hipLaunchKernelGGL((append_e4m3_kernel<decltype(dp)::value, decltype(m)::value>), dim3(grid), dim3(kThreads), kBlockTokens * angles, stream, p, kv_wgs,
+                       heads_per_wg, tokens_per_wg);
   };
   auto with_width = [&](auto dp) {
-    if (mode == kNone) with_mode(dp, attn::Tag<kNone>{});
-    else if (mode == kHalves) with_mode(dp, attn::Tag<kHalves>{});
-    else if (mode == kWhole) with_mode(dp, attn::Tag<kWhole>{});
-    else if (mode == kNeighbours) with_mode(dp, attn::Tag<kNeighbours>{});
-    else with_mode(dp, attn::Tag<kAnywhere>{});
+    if (decltype(dp)::value > 64 && mode == kHalves && half == decltype(dp)::value / 2) launch(dp, attn::Tag<kWhole>{});
+    else with_mode([&](auto m) { launch(dp, m); });
   };
   if (p.head_dim <= 64) with_width(attn::Tag<64>{});
   else if (p.head_dim <= 128) with_width(attn::Tag<128>{});
