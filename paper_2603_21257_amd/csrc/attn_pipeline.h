@@ -131,10 +131,10 @@ struct WinPipe8Cfg : WinPipeCfg<NW_, RING_, HB_> {
   static constexpr int VA = 4;                         // the drain's V is stored by the last steady step
   static constexpr bool E8 = true;
 };
-// 0, 2, 3, 1.  A 16-byte LDS read serves, at a time, rows c / 4 = 0 and 3 of one g and 1 and 2 of the next, or the other way round: with row r's chunks at
+// 0, 3, 2, 1.  A 16-byte LDS read serves, at a time, rows c / 4 = 0 and 3 of one g and 1 and 2 of the next, or the other way round: with row r's chunks at
 // g ^ r those share banks, with these they do not: 32 conflict cycles less a step and wave, of 64 (the stores count the others; 28096+28, 28304+61 and
 // 38304+209 tokens, 32Q/8KV, 171 / 170 us a call).
-__device__ inline int v_swizzle(int r) { return 0x78 >> 2 * r & 3; }
+__device__ inline int v_swizzle(int r) { return -r & 3; }
 // WIN: the reference of a row that has seen no key.  Finite, so that the weight of a hidden key (score -inf) is 0 against it; far enough below
 // every score for the first visible one to pass the bound.
 constexpr float kNoRef = -3e38f;
