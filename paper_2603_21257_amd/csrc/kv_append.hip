@@ -439,8 +439,11 @@ hipError_t launch_kv_append(const KvAppendParams& p, int dtype, int n_cus, hipSt
   using namespace append;
   if (p.total_tokens <= 0 || (!p.q && !p.k)) return hipSuccess;
   const int half = p.rope.half, per_chunk = dtype == CALVO_F32 ? 4 : 8;
-  // a workgroup's tokens share their angles' start-up; few tokens are spread over the chip
-  const int tokens_per_wg = p.total_tokens >= 16 * n_cus ? kMostTokens : 1;
+  // Several tokens share a workgroup's start where there are many and their rows leave its threads few chunks each.  One / four to a workgroup, us of the launch:
+  // bf16, 8000 tokens, 8Q/8KV, D = 64 13.8 / 11.6, 32Q/8KV 20.4 / 18.6, D = 128 32.5 / 33.0, D = 256 76.5 / 83.7; 600 tokens, D = 128 6.1 / 10.6
+  const bool many = p.total_tokens >= 16 * n_cus;
+  const int row_chunks = ((p.q ? p.n_q_heads : 0) + (p.k && dtype != CALVO_E4M3 ? 2 * p.n_kv_heads : 0)) * p.head_dim / per_chunk;
+  const int tokens_per_wg = many && row_chunks <= 2 * kThreads ? kMostTokens : 1;
   const unsigned row_wgs = (unsigned)((p.total_tokens + tokens_per_wg - 1) / tokens_per_wg);
   const size_t angles = (size_t)angle_row(half) * sizeof(attn::f32x2);
   const int mode = p.rope.rot == 0 ? kNone : p.rope.interleaved ? kNeighbours : half % per_chunk ? kAnywhere : kHalves;
@@ -458,12 +461,14 @@ hipError_t launch_kv_append(const KvAppendParams& p, int dtype, int n_cus, hipSt
     });
     return hipGetLastError();
   }
-  // a wave for each K and V of a head where blocks are few; else a block's angles are made once for eight heads
-  const int heads_per_wg = (int64_t)p.n_touched * p.n_kv_heads <= 8 * n_cus ? 2 : 8;
+  // a wave for each K and V of a head where blocks are few; else a block's angles are made once for eight heads (two / eight, 32Q/8KV, D = 128: 1 token 4.0 / 7.4,
+  // 1000 8.3 / 11.2, 4000 23.7 / 20.4; 8Q/8KV, D = 64, 2000 tokens 7.2 / 9.8)
+  const int heads_per_wg = (int64_t)p.n_touched * p.n_kv_heads <= 4 * n_cus ? 2 : 8;
   const int groups = (p.n_kv_heads + heads_per_wg - 1) / heads_per_wg;
   const int kv_wgs = p.k ? p.n_touched * groups : 0;
-  // Many rows of q go by themselves: beside the blocks they would have half the waves to a CU
-  const bool apart = p.q && kv_wgs && tokens_per_wg > 1;
+  // Many wide rows of q go by themselves: beside the blocks of such heads they would have two waves to a SIMD (8000 tokens, 32Q/8KV, a launch of their own / one
+  // launch: D = 256 83 / 114, D = 128 36.5 / 33.9, D = 64 24.8 / 19.4)
+  const bool apart = p.q && kv_wgs && many && p.head_dim > 128;
   if (apart)
     with_mode([&](auto m) {
       hipLaunchKernelGGL(append_q_kernel<decltype(m)::value>, dim3(row_wgs), dim3(kThreads), tokens_per_wg * angles, stream, p, tokens_per_wg);
