@@ -435,8 +435,8 @@ auto with_cfg(int head_dim, int tile_rows, F&& f) {
   if (head_dim == 64) return tile_rows == 16 ? f(Cfg<64, 1, 4, true>{}) : f(Cfg<64, 2, 4, true>{});
   if (head_dim < 64) return tile_rows == 16 ? f(Cfg<64, 1, 4, false>{}) : f(Cfg<64, 2, 4, false>{});
   if (head_dim < 128) return tile_rows == 16 ? f(Cfg<128, 1, 4, false>{}) : f(Cfg<128, 2, 4, false>{});
-  if (head_dim == 256) return f(Cfg<256, 1, 4, true>{});
-  return f(Cfg<256, 1, 4, false>{});
+  if (head_dim == 256) return tile_rows == 16 ? f(Cfg<256, 1, 4, true>{}) : f(Cfg<256, 2, 4, true>{});
+  return tile_rows == 16 ? f(Cfg<256, 1, 4, false>{}) : f(Cfg<256, 2, 4, false>{});
 }
 
 }  // namespace e4m3

@@ -125,9 +125,10 @@ RowsShape e4m3_shape(int head_dim, bool few, bool large) {
   const int step = head_dim <= 64 ? 8 : head_dim <= 128 ? 13 : 24;
   if (few) return {kFewRows, step, 20, 1};
   // Wider heads are cut earlier (60 / 45, D = 256: 700+60 tokens, 8Q/2KV 13.5 / 12.0, 500+33, 4Q/4KV 12.1 / 11.4, nine other shapes the same); with 45
-  // 128-wide ones would stay on packed rows too rarely (4096+64 behind 1024, 32Q/8KV 10.0 / 14.7)
-  const int start = head_dim > 128 ? 45 : 60;
-  return large ? RowsShape{32, step + step / 2, start, 1} : RowsShape{kFewRows, step, start, 1};
+  // 128-wide ones would stay on packed rows too rarely (4096+64 behind 1024, 32Q/8KV 10.0 / 14.7).  Their tiles of 32 rows cost little more a step, whose time goes
+  // to widening, and more to end (16 / 32 rows, D = 256: 8192+1024, 32Q/8KV 662 / 389, 2000+200, 8Q/2KV 22.0 / 21.0, 5000+30 15.3 / 17.8, 700+60 12.0 / 15.2)
+  if (head_dim > 128) return large ? RowsShape{32, 29, 75, 1} : RowsShape{kFewRows, step, 45, 1};
+  return large ? RowsShape{32, step + step / 2, 60, 1} : RowsShape{kFewRows, step, 60, 1};
 }
 
 // The launch of the chosen candidate; a packed-rows workgroup merges at most merge_rows rows along (plan_window)
@@ -163,7 +164,7 @@ void plan_window_e4m3(const WindowShape& s, const std::vector<WindowLens>& lens,
   for (const WindowLens& l : lens) few &= (int64_t)l.n_new * group <= kFewRows;
   Candidate best;
   for (const bool large : {false, true}) {
-    if (large && (few || s.head_dim > 128 || s.force_tile == 1)) break;
+    if (large && (few || s.force_tile == 1)) break;
     Candidate c;
     c.unit = kE4m3Keys;
     c.shape = e4m3_shape(s.head_dim, few, large);
