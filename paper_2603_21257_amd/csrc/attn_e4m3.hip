@@ -7,8 +7,8 @@
 // the pool straight to the registers of the lanes whose operands they are, no LDS and no barrier until the waves add their rows at the end.
 //
 // Single tokens are bound by the bytes: 32 requests of 300 to 33000 tokens, 32Q/8KV, D = 128, 477 MB a layer in 90 us, 5.3 TB/s; short contexts by a chain of
-// waits (descriptor, table, K, V, the waves' sum, the merge): 4096+1 tokens 7.2 us.  Many rows by the vector ALU, which widens K and V for 32 rows only (16 behind
-// 128-wide heads): 16384+2048 tokens 387 us with D = 64, 755 TFLOP/s; 8192+1024 with D = 256 662 us, 441 TFLOP/s; 128-wide heads with many rows run on
+// waits (descriptor, table, K, V, the waves' sum, the merge): 4096+1 tokens 7.2 us.  Many rows by the vector ALU, which widens K and V for 32 rows only:
+// 16384+2048 tokens with D = 64 387 us, 755 TFLOP/s; 8192+1024 with D = 256 389 us, 752 TFLOP/s (16 rows: 662 us).  128-wide heads with many rows run on
 // attn_e4m3_pipe.hip.  Long contexts of few rows are cut into pieces (window_plan.cpp).
 #include "attn_rows_body.h"
 #include "kv_e4m3.h"
@@ -34,6 +34,7 @@ struct Cfg {
   static constexpr int LDS_BYTES = LDS_O + NW * ROWS * 8;
 };
 
+// Two waves to a SIMD; wider heads have its 512 registers to themselves
 template <class C>
 __global__ void __launch_bounds__(64 * C::NW, C::DP > 128 ? 1 : 2) attn_e4m3_kernel(WinParams p) {
   constexpr int DP = C::DP, QB = C::QB, NW = C::NW, KJ = C::KJ, DB = C::DB;
