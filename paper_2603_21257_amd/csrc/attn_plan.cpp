@@ -157,7 +157,7 @@ int plan_pieces(const std::vector<PlanTile>& tiles, const PlanParams& p, int64_t
   }
   FreeSlots heap;
   for (int n : p.long_pieces ? coarse : all) {
-    if (n > 1 && wgs * n > (p.step_cost ? 4 : 16) * (int64_t)p.wg_slots) break;
+    if (p.most ? n > p.most : n > 1 && wgs * n > (p.step_cost ? 4 : 16) * (int64_t)p.wg_slots) break;
     bool cut = false;
     int64_t end = 0, slots = 0, work = 0, longest = 0;
     for (const auto& [n_sub, wgs_of] : runs) {
@@ -168,7 +168,7 @@ int plan_pieces(const std::vector<PlanTile>& tiles, const PlanParams& p, int64_t
       work += ((np - 1) * cost_of(len) + cost_of(n_sub - (np - 1) * len)) * wgs_of;
       longest = std::max(longest, cost_of(std::min(len, n_sub)));
     }
-    if (n > 1 && slots > max_slots) break;
+    if (n > 1 && (slots > max_slots || (p.most && slots > 4 * (int64_t)p.wg_slots))) break;
     // no order of the pieces beats the average load or the longest piece: most candidates need no replay
     const double step = slots <= p.alone ? kAlone : 1.;
     const double merge = (cut ? 1. : 1. - step) * p.split_fill;

@@ -120,10 +120,12 @@ void choose_pipelined(const WindowShape& s, const std::vector<WindowLens>& lens,
 // its reads (1.3 us while they leave the memory's rate alone), and the last piece of a tile to arrive merges them in 1.7 us a round of 32.  us a call of
 // one caller, 32Q/8KV, D = 128, with launches of half, one and two workgroups to a CU in mind: 8 requests of 500 to 20000 behind 4096 17.8 / 13.1 / 13.8,
 // four of 4096 12.9 / 10.5 / 12.0, 32 of 300 to 33000 138.7 / 112.3 / 109.9, 60000+1 28.1 / 25.2 / 25.2, 24 of 3000 40.4 / 37.1 / 40.4.
-constexpr int kMostMerged = 32;
-RowsShape e4m3_shape(int head_dim, bool few, bool large) {
+constexpr int kMostMerged = 32, kMergedAlong = 4;              // pieces; rows, a wave each
+RowsShape e4m3_shape(int head_dim, bool few, bool large, bool along) {
   const int step = head_dim <= 64 ? 8 : head_dim <= 128 ? 13 : 24;
-  if (few) return {kFewRows, step, 20, 1};
+  // A merge in a launch of its own costs twice as much (20 / 40: 7524+1 and seven shorter behind 528, 16Q/2KV, D = 96 9.6 / 7.5, 20 + 1 to 34792 + 1 behind 316, 40Q/8KV,
+  // D = 128 9.0 / 7.6, 40 drawn batches 1 % less)
+  if (few) return {kFewRows, step, along ? 20 : 40, 1};
   // Wider heads are cut earlier (60 / 45, D = 256: 700+60 tokens, 8Q/2KV 13.5 / 12.0, 500+33, 4Q/4KV 12.1 / 11.4, nine other shapes the same); with 45
   // 128-wide ones would stay on packed rows too rarely (4096+64 behind 1024, 32Q/8KV 10.0 / 14.7).  Their tiles of 32 rows cost little more a step, whose time goes
   // to widening, and more to end (16 / 32 rows, D = 256: 8192+1024, 32Q/8KV 662 / 389, 2000+200, 8Q/2KV 22.0 / 21.0, 5000+30 15.3 / 17.8, 700+60 12.0 / 15.2)
@@ -160,25 +162,32 @@ void make_plan(const WindowShape& s, const std::vector<WindowLens>& lens, int32_
 
 void plan_window_e4m3(const WindowShape& s, const std::vector<WindowLens>& lens, int32_t window, int32_t n_first, WindowPlan& out) {
   const int group = s.n_q_heads / s.n_kv_heads;
-  bool few = s.force_tile == 0;
-  for (const WindowLens& l : lens) few &= (int64_t)l.n_new * group <= kFewRows;
+  bool few = s.force_tile == 0, along = true;
+  for (const WindowLens& l : lens) {
+    few &= (int64_t)l.n_new * group <= kFewRows;
+    along &= (int64_t)l.n_new * group <= kMergedAlong;
+  }
   Candidate best;
   for (const bool large : {false, true}) {
     if (large && (few || s.force_tile == 1)) break;
     Candidate c;
     c.unit = kE4m3Keys;
-    c.shape = e4m3_shape(s.head_dim, few, large);
+    c.shape = e4m3_shape(s.head_dim, few, large, along);
     c.params = rows_plan_params(c.shape, s.n_kv_heads, few || s.head_dim > 128 ? s.n_cus : 2 * s.n_cus, s.force_splits);
+    // 24 single tokens, 32Q/8KV, D = 128, of which one has 47862 cached tokens and most have few: pieces counted as if all were cut / as many as come of it
+    // 60.6 / 36.0 us a call; 8Q/8KV, D = 96, 46902 39.7 / 24.5; even batches the same, chunks too
+    if (few) c.params.most = kMostMerged;
     make_tiles(c, lens, group, window, n_first);
     c.want = plan_pieces(c.tiles, c.params, kMostSlots / c.shape.slots, &c.cost);
-    if (few && !s.force_splits) c.want = std::min(c.want, kMostMerged);
     if (best.tiles.empty() || (large && s.force_tile == 2) || c.cost.span < best.cost.span) best = std::move(c);
   }
-  // Where the replays' lengths differ by 2.4 (packed rows in tenths of a microsecond, the pipelined kernels in steps) the two take the same time.  us a call of
-  // one caller, 32Q/8KV, packed rows / kAttnDuo, and that quotient: 4096+64 behind 1024 10.1 / 25.0 (2.4), 1000+100 10.5 / 26.1 (2.3), 60000+5 36.2 / 41.4
-  // (2.1), 0+500 16.7 / 15.6 (2.4), 20000+8 28.7 / 22.5 (2.4), 20000+16 35.2 / 23.5 (2.7), 20000+64 44.2 / 35.7 (3.9), 4096+256 44.8 / 34.3 (3.7).
-  if (s.head_dim == 128 && s.force_variant != 5 && !few) choose_pipelined(s, lens, window, n_first, 0.248 * best.cost.span, best);
-  make_plan(s, lens, window, n_first, best, 4, out);
+  // Where the replays' lengths differ by 2.4 (packed rows in tenths of a microsecond, the pipelined kernels in steps) the two take the same time, but for 9 us that
+  // the start, end and merge of the latter take more.  us a call of one caller, 32Q/8KV, packed rows / kAttnDuo, and that quotient: 4096+64 behind 1024
+  // 10.1 / 25.0 (2.4), 1000+100 10.5 / 26.1 (2.3), 60000+5 36.2 / 41.4 (2.1), 20000+16 35.2 / 23.5 (2.7), 20000+64 44.2 / 35.7 (3.9), 4096+256 44.8 / 34.3 (3.7);
+  // few heads or long and short requests in one batch: 0+1015 and 45+1, 8Q/8KV 12.0 / 25.4, 1543+435, 6Q/3KV 14.1 / 23.4, 330+259 and 413+215 14.7 / 18.6.
+  constexpr double kPipelinedStart = 9.;
+  if (s.head_dim == 128 && s.force_variant != 5 && !few) choose_pipelined(s, lens, window, n_first, 0.248 * best.cost.span - kPipelinedStart, best);
+  make_plan(s, lens, window, n_first, best, kMergedAlong, out);
 }
 
 }  // namespace
