@@ -156,7 +156,8 @@ int plan_pieces(const std::vector<PlanTile>& tiles, const PlanParams& p, int64_t
     runs.back().second += p.n_head_groups;
   }
   FreeSlots heap;
-  for (int n : p.long_pieces ? coarse : all) {
+  // `most` looks at more counts; where many tiles make each replay long, at the coarse ones (32 single tokens of 300 to 33000 32 / 27 us of host time a plan, launches the same)
+  for (int n : p.long_pieces || (p.most && 4 * wgs > p.wg_slots) ? coarse : all) {
     if (p.most ? n > p.most : n > 1 && wgs * n > (p.step_cost ? 4 : 16) * (int64_t)p.wg_slots) break;
     bool cut = false;
     int64_t end = 0, slots = 0, work = 0, longest = 0;

@@ -130,7 +130,12 @@ RowsShape e4m3_shape(int head_dim, bool few, bool large, bool along) {
   // 128-wide ones would stay on packed rows too rarely (4096+64 behind 1024, 32Q/8KV 10.0 / 14.7).  Their tiles of 32 rows cost little more a step, whose time goes
   // to widening, and more to end (16 / 32 rows, D = 256: 8192+1024, 32Q/8KV 662 / 389, 2000+200, 8Q/2KV 22.0 / 21.0, 5000+30 15.3 / 17.8, 700+60 12.0 / 15.2)
   if (head_dim > 128) return large ? RowsShape{32, 29, 75, 1} : RowsShape{kFewRows, step, 45, 1};
-  return large ? RowsShape{32, step + step / 2, 60, 1} : RowsShape{kFewRows, step, 60, 1};
+  if (large) return {32, step + step / 2, 60, 1};
+  // Tiles of 16 rows of narrow heads have 126 registers: four workgroups to a CU, whose steps take the longer.  us a call of one caller, D = 64, as two at 8 and 60 /
+  // as four at 15 and 45: 787+7218 behind 24, 32Q/8KV 71.1 / 51.5, 257+1643 behind 41, 64Q/8KV 33.0 / 25.5, 0+1032, 40Q/8KV 21.1 / 18.6, 4142+24 with 207+633, 16Q/4KV 12.8 / 12.7;
+  // 60 drawn batches 5 % less
+  if (head_dim <= 64) return {kFewRows, 15, 45, 1};
+  return {kFewRows, step, head_dim < 128 ? 50 : 60, 1};
 }
 
 // The launch of the chosen candidate; a packed-rows workgroup merges at most merge_rows rows along (plan_window)
@@ -173,10 +178,12 @@ void plan_window_e4m3(const WindowShape& s, const std::vector<WindowLens>& lens,
     Candidate c;
     c.unit = kE4m3Keys;
     c.shape = e4m3_shape(s.head_dim, few, large, along);
-    c.params = rows_plan_params(c.shape, s.n_kv_heads, few || s.head_dim > 128 ? s.n_cus : 2 * s.n_cus, s.force_splits);
+    const int per_cu = few || s.head_dim > 128 ? 1 : s.head_dim <= 64 && !large ? 4 : 2;
+    c.params = rows_plan_params(c.shape, s.n_kv_heads, per_cu * s.n_cus, s.force_splits);
+    if (per_cu == 4) c.params.alone = s.n_cus;               // 2737+113 behind 1500, 32Q/8KV: without / with 14.0 / 8.4
     // 24 single tokens, 32Q/8KV, D = 128, of which one has 47862 cached tokens and most have few: pieces counted as if all were cut / as many as come of it
-    // 60.6 / 36.0 us a call; 8Q/8KV, D = 96, 46902 39.7 / 24.5; even batches the same, chunks too
-    if (few) c.params.most = kMostMerged;
+    // 60.6 / 36.0 us a call; 8Q/8KV, D = 96, 46902 39.7 / 24.5; 53091+1 with 0+817, 16Q/4KV, D = 64 53.6 / 15.4; even batches the same
+    c.params.most = kMostMerged;
     make_tiles(c, lens, group, window, n_first);
     c.want = plan_pieces(c.tiles, c.params, kMostSlots / c.shape.slots, &c.cost);
     if (best.tiles.empty() || (large && s.force_tile == 2) || c.cost.span < best.cost.span) best = std::move(c);
