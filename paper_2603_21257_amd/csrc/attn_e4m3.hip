@@ -208,8 +208,8 @@ __global__ void __launch_bounds__(64 * C::NW, C::DP > 128 ? 1 : 2) attn_e4m3_ker
 #pragma unroll
         for (int db = 0; db < DB; db++) o[qb][db] *= alpha[qb];
     }
-    if (hides) {                                               // NaN in V: the product takes weight 0 times it, also for rows that do not see the key
-      dirty |= not_finite(vs[A]) ? 1u : 0u;
+    if (hides) {                                               // NaN or an infinity in V: the product takes weight 0 times it, also for rows that do not see the key
+      dirty |= may_not_be_finite(vs[A]) ? 1u : 0u;
 #pragma unroll
       for (int db = 0; db < DB; db++)
 #pragma unroll

@@ -45,7 +45,8 @@ __device__ inline unsigned pack4(float a, float b, float c, float d) {
 
 // bytes that are NaN (0x7f, 0xff), marked in their upper bits
 __device__ inline unsigned nan_bytes(unsigned x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
-__device__ inline bool not_finite(float s) { return (bits_of(s) & 0x7f800000u) == 0x7f800000u; }
+// scales from 2^120 on, against which bytes of 256 and more are infinite in bf16, and those that are NaN themselves
+__device__ inline bool may_not_be_finite(float s) { return (bits_of(s) & 0x7f800000u) >= (247u << 23); }
 
 }  // namespace e4m3
 }  // namespace calvo
