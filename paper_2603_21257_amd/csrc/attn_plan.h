@@ -39,7 +39,7 @@ struct PlanParams {
   int step_cost = 0;  // packed-rows kernel: cost of a wave's 32-key step, in units of split_fill; else 0
   int alone = 0;      // > 0: up to this many workgroups have a CU each, which makes them faster (attn_plan.cpp)
   bool rounded = false;   // piece lengths of the form 8k + 2 instead of even ones
-  int most = 0;           // > 0: up to this many pieces for the longest tile, also where others are many but too short to be cut; limited are the pieces that come of it
+  int most = 0;           // > 0: up to this many pieces for the longest tile, also where others are many but too short to be cut; limited are the pieces of cut tiles, not the uncut ones beside them
 };
 
 // A work item is one workgroup's share of the attention of one request: a tile of suffix tokens

@@ -288,7 +288,7 @@ int window_prepare(calvo_ctx* c, const calvo_window_request* reqs, int n_reqs, i
   size_t n_offs = 0;
   for (int r = 0; r < n_reqs && !rows; r++) n_offs += (size_t)offs_of(((int64_t)reqs[r].n_cached + reqs[r].n_new + kBlockTokens - 1) / kBlockTokens);
   const size_t words = pad4(w->offs_at + 2 * n_offs);
-  const size_t pieces = w->plan.split_tiles.empty() ? 0 : n_items * (size_t)w->plan.part_rows;
+  const size_t pieces = (size_t)w->plan.n_parts * (size_t)w->plan.part_rows;
   w->part_o_at = (words + 63) / 64 * 64;
   w->part_ml_at = w->part_o_at + pieces * (size_t)w->plan.part_width;
   w->part_mass_at = w->part_ml_at + pieces * 2;

@@ -159,6 +159,7 @@ void make_plan(const WindowShape& s, const std::vector<WindowLens>& lens, int32_
   }
   const PlanItems pi = plan_items(best.tiles, best.want, best.params);
   out.split_tiles = pi.split_tiles;
+  if (!pi.split_tiles.empty()) out.n_parts = pi.split_tiles.back() + pi.items[(size_t)pi.split_tiles.back()].n_splits;   // the longest tiles come first
   out.items.reserve(pi.items.size());
   for (const WorkItem& x : pi.items)
     out.items.push_back({x.req, x.q_tile, x.sub_begin, x.sub_end, x.n_splits, x.first_item,

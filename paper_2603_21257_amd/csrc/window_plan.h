@@ -39,6 +39,7 @@ struct WindowPlan {
   int64_t part_rows = 0, part_width = 0; // rows of partial results that a work item leaves over all heads, floats of one
   std::vector<WindowPiece> items;
   std::vector<int32_t> split_tiles;      // first item of every cut tile
+  int64_t n_parts = 0;                   // items up to the last one of a cut tile: those that partial results have room for
 };
 
 constexpr int kFewRows = 16;             // tile_rows for single tokens
