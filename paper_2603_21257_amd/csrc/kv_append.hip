@@ -485,8 +485,10 @@ hipError_t launch_kv_append(const KvAppendParams& p, int dtype, int n_cus, hipSt
                        heads_per_wg, tokens_per_wg);
   };
   auto with_width = [&](auto dp) {
-    if (decltype(dp)::value > 64 && mode == kHalves && half == decltype(dp)::value / 2) launch(dp, attn::Tag<kWhole>{});
-    else with_mode([&](auto m) { launch(dp, m); });
+    if constexpr (decltype(dp)::value > 64) {                  // a lane of narrower heads has no chunk of its other half
+      if (mode == kHalves && half == decltype(dp)::value / 2) return launch(dp, attn::Tag<kWhole>{});
+    }
+    with_mode([&](auto m) { launch(dp, m); });
   };
   if (p.head_dim <= 64) with_width(attn::Tag<64>{});
   else if (p.head_dim <= 128) with_width(attn::Tag<128>{});
