@@ -116,7 +116,7 @@ typedef struct {
 int calvo_block_bytes(const calvo_config* cfg, int64_t* bytes);
 
 /* Create a context for one pool.  Allocates the staging ring, one event per layer, room for the partial
- * results of cut contexts (68 MB for bf16 pools of head dim 128, 34 MB for others) and
+ * results of cut contexts (68 MB for bf16 pools of head dim 128, none for CALVO_E4M3, 34 MB for others) and
  * the internal streams on the current device.  CALVO_EINVAL for a bad shape or NULL pool,
  * CALVO_ENOMEM / CALVO_EHIP if a device resource cannot be obtained (nothing is leaked). */
 int calvo_create(const calvo_config* cfg, calvo_ctx** out);

@@ -660,7 +660,7 @@ int calvo_create(const calvo_config* cfg, calvo_ctx** out) {
       e = attn_rows_prepare(cfg->dtype, cfg->head_dim, attn_rows_shape(f32, cfg->head_dim, true).tile_rows);
     if (e != hipSuccess) { const int prc = fail_hip(e, "hipFuncSetAttribute(dynamic LDS)"); destroy_partial(c); return prc; }
   }
-  {
+  if (cfg->dtype != CALVO_E4M3) {                              // the calls that leave partial results there refuse such a pool
     const bool mfma = cfg->dtype == CALVO_BF16 && cfg->head_dim == 128;
     const int prc = ensure_partials(c, mfma ? kPartialSlots0 : kStaticPartSlots);
     if (prc != CALVO_OK) { destroy_partial(c); return prc; }
