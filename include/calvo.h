@@ -33,8 +33,9 @@
  *    K [Hkv][B][D] bytes, V [Hkv][D][B] bytes, scales fp32 [K, V][Hkv], and room up to a multiple of 128 bytes (calvo_block_bytes)
  * A byte is an 8-bit float of the OCP format E4M3 (four bits of exponent, three of fraction, largest 448, no infinity, 0x7f and 0xff NaN) and
  * stands for its value times the scale of its K or V, block and head.  A scale is a power of two, 2^-126 to 2^120: only its exponent is looked at;
- * one that is not finite makes all its values NaN.  What a byte stands for is read as bf16 would hold it: below 2^-126 it may be zero, from 2^128 on it is infinite.  Loading moves such blocks as any others, at half the bytes of bf16; calvo_window_prepare,
- * calvo_kv_append, calvo_window_attn and the calls without a pool take them, the others refuse with CALVO_EINVAL.
+ * one that is not finite makes all its values NaN.  What a byte stands for is read as bf16 would hold it: below 2^-126 it may be zero, from 2^128 on it
+ * is infinite.  Loading moves such blocks as any others, at half the bytes of bf16; calvo_window_prepare, calvo_kv_append, calvo_window_attn and the calls
+ * without a pool take them, the others refuse with CALVO_EINVAL.
  * The paper names blocks, tiers and the context/query split but no block size,
  * layout or precision; these are this library's definitions.
  *
@@ -327,7 +328,8 @@ int calvo_window_destroy(calvo_window* w);
  * lse: DEVICE fp32 [new tokens][Hq] or NULL.  Element type, accumulation, rounding and scale as calvo_prefill_attn; one kernel serves the batch, so
  * the last bits of a request's results may depend on the requests beside it.  K and V of
  * positions that a row does not see never reach its results, whatever they hold; nor does what lies behind a request's last
- * token in its last slot.  Can be captured into a graph (k_new and v_new included): a captured call cannot wait for a load and gets
+ * token in its last slot.  (A scale of a CALVO_E4M3 pool belongs to all tokens of its block and head: one that calvo_kv_append left as NaN, for a new value
+ * that was not finite, makes NaN of each of them, so that rows that see any of these are NaN, whether they see that value's token or not.)  Can be captured into a graph (k_new and v_new included): a captured call cannot wait for a load and gets
  * CALVO_ENOTREADY while one is under way.  Errors (nothing queued): CALVO_EINVAL for a bad layer, NULL or misaligned pointers, out, lse or the
  * layer's pool overlapping each other or an input. */
 int calvo_window_attn(calvo_window* w, int layer, const void* q, const void* k_new, const void* v_new, void* out, float* lse, float scale);
@@ -351,7 +353,8 @@ typedef struct {
  * CALVO_E4M3 pools: q, k_new and v_new are bf16, rotated K is quantised as it comes out of the sum.  A block that takes new tokens is written whole: its
  * scale (K and V, per head) becomes the smallest power of two s for which every new value is at most 448 s, but not less than that of the tokens it holds
  * already; where the scale grows these are rounded again to the larger one (exact, but for values below 2^-6 of it); room behind the last token becomes zeros.  A
- * NaN or an infinity among the new values makes that scale NaN: all values of the block and head read as NaN.
+ * NaN or an infinity among the new values (of K: as rotated, in fp32) makes that scale NaN: all values of the block and head, those of the tokens that it held
+ * already among them, read as NaN from then on.  Pools of bf16 and fp32 hold such a value like any other.
  * Can be captured, as calvo_window_attn.  Errors (nothing queued): CALVO_EINVAL for a bad layer, misaligned pointers (16 bytes), strides below a row or that
  * are not whole 16 bytes, a rope outside the limits above, q_out or the layer's pool overlapping each other or an input. */
 int calvo_kv_append(calvo_window* w, int layer, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const void* q, int64_t q_stride,

@@ -1,10 +1,12 @@
 // Attention over a pool of 8-bit floats with a scale for each block and head (calvo_window_attn on CALVO_E4M3 pools), packed rows: any head width, any
 // group size, single tokens to chunks.
 //
-// out = sum_t exp(s_t - m) V_t / sum_t exp(s_t - m) in one pass with the running maximum m and sum of a row; a tile's rows are the (token, query head) pairs of a
-// KV head, 16 or 32 of them.  Both products take bf16 operands: K and V are widened in registers with their scale, which is exact, and weights are rounded
-// once to bf16.  (Products of 8 bits would round q and the weights to four bits.)  A wave takes every fourth step of 64 keys of the tile by itself: K and V go from
-// the pool straight to the registers of the lanes whose operands they are, no LDS and no barrier until the waves add their rows at the end.
+// out = sum_t exp(s_t - m) V_t / sum_t exp(s_t - m) in one pass with the running maximum m and sum of a row; a tile's rows are the (token, query head) pairs of
+// a KV head, 16 or 32 of them.  Both products take bf16 operands: K and V are widened in registers with their scale, which is exact, and weights are rounded
+// once to bf16: outputs are 1.64e-3 to 1.76e-3 (2-norm, relative) off 64 bits, of which 1.6e-3 is their own rounding, and the three terms to a weight that the
+// packed rows over bf16 pools take would be three products instead of one.  (Products of 8 bits would round q and the weights to four bits.)  A wave takes
+// every fourth step of 64 keys of the tile by itself: K and V go from the pool straight to the registers of the lanes whose operands they are, no LDS and no
+// barrier until the waves add their rows at the end.
 //
 // Single tokens are bound by the bytes: 32 requests of 300 to 33000 tokens, 32Q/8KV, D = 128, 477 MB a layer in 90 us, 5.3 TB/s; short contexts by a chain of
 // waits (descriptor, table, K, V, the waves' sum, the merge): 4096+1 tokens 7.2 us.  Many rows by the vector ALU, which widens K and V for 32 rows only:
@@ -275,7 +277,7 @@ __global__ void __launch_bounds__(64 * C::NW, C::DP > 128 ? 1 : 2) attn_e4m3_ker
       if (left == 2) step(st + NW, Tag<1>{}, Tag<0>{});
     }
   }
-  // With such V the wave's rows meet its keys again, 16 at a time and V key by key: a row adds weight times V of the keys that it sees and touches no
+  // With such V (a byte or a scale that is NaN, a scale against which some bytes are infinite) the wave's rows meet its keys again, 16 at a time and V key by key: a row adds weight times V of the keys that it sees and touches no
   // other.  Rare, so it is written for few registers.
   if (__builtin_expect(__builtin_amdgcn_ballot_w64(dirty != 0) != 0, 0)) {
     static_for<0, QB>([&](auto qb_tag) __attribute__((always_inline)) {

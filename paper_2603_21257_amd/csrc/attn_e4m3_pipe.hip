@@ -1,8 +1,9 @@
-// Attention over a pool of 8-bit floats on the pipelined bodies (attn_pipeline.h, WinPipe8Cfg): 128-wide heads, tiles of many rows.  K and V are widened
-// once for a workgroup, on their way into LDS, and from there on all is as over a bf16 pool.  32Q/8KV: 16384+2048 tokens 433 us, 1350 TFLOP/s, 0+16384 1620 us,
-// 1360 (a large library product 1400): power, as over bf16 pools, which take the same time and twice the memory.  Short queries (28096+28, 28304+61,
-// 38304+209) 170 us, 1015: rows of tiles that tokens do not fill, starts and ends of pieces, and 8 us of merging.  256 registers and 133 accumulation registers: with
-// 240 the compiler moved results of products between the two.
+// Attention over a pool of 8-bit floats on the pipelined bodies (attn_pipeline.h, WinPipe8Cfg): 128-wide heads, tiles of many rows.  K and V are widened once
+// for a workgroup, on their way into LDS, and from there on all is as over a bf16 pool.  32Q/8KV, calls queued back to back: 16384+2048 tokens 433 us, 1350
+// TFLOP/s for one caller whose clock has come up, 431 to 441 for several in turn, 0+16384 1620 us (1360) and 1654 to 1718 (1280 to 1330; a large library
+// product 1400): power, as over bf16 pools, which take the same time and twice the memory.  Short queries (28096+28, 28304+61, 38304+209) 170 us, 1015: rows of
+// tiles that tokens do not fill, starts and ends of pieces, and 8 us of merging.  256 registers and 133 accumulation registers: with 240 the compiler moved
+// results of products between the two.
 #include "attn_merge.h"
 #include "attn_pipeline.h"
 

@@ -9,8 +9,8 @@
 // of 16 bytes a lane, a workgroup to a token or four, whose angles it makes once into LDS.  Into an 8-bit pool a block is written whole, since its scale
 // depends on all of its tokens: a wave has K or V of one (block, head) in registers, finds the largest value, and stores bytes in the order that attention
 // reads (K by token; V by element, so that a lane has two elements of all 16 tokens and turns nothing around).  What a block holds already is asked for with the
-// new values.  us of a call, 32Q/8KV, D = 128, all of a head rotated: 8000 tokens bf16 31.7 (6.2 TB/s), fp32 74.6 (5.3), 8 bits 32.7 (5.5); 32 requests of one
-// token 4.8, a single one 3.9.
+// new values.  us of a call, 32Q/8KV, D = 128, all of a head rotated: 8000 tokens bf16 31.7 (6.2 TB/s), fp32 74.6 (5.3), 8 bits 31.5 (5.7); 32 requests of one
+// token 4.6, a single one 4.6 (of the kernel 4.5 and 3.8).
 #include "../../include/calvo.h"
 #include "kv_e4m3.h"
 

@@ -124,7 +124,7 @@ constexpr int kMostMerged = 32, kMergedAlong = 4;              // pieces; rows, 
 RowsShape e4m3_shape(int head_dim, bool few, bool large, bool along) {
   const int step = head_dim <= 64 ? 8 : head_dim <= 128 ? 13 : 24;
   // A merge in a launch of its own costs twice as much (20 / 40: 7524+1 and seven shorter behind 528, 16Q/2KV, D = 96 9.6 / 7.5, 20 + 1 to 34792 + 1 behind 316, 40Q/8KV,
-  // D = 128 9.0 / 7.6, 40 drawn batches 1 % less)
+  // D = 128 9.0 / 7.6)
   if (few) return {kFewRows, step, along ? 20 : 40, 1};
   // Wider heads are cut earlier (60 / 45, D = 256: 700+60 tokens, 8Q/2KV 13.5 / 12.0, 500+33, 4Q/4KV 12.1 / 11.4, nine other shapes the same); with 45
   // 128-wide ones would stay on packed rows too rarely (4096+64 behind 1024, 32Q/8KV 10.0 / 14.7).  Their tiles of 32 rows cost little more a step, whose time goes
@@ -132,8 +132,7 @@ RowsShape e4m3_shape(int head_dim, bool few, bool large, bool along) {
   if (head_dim > 128) return large ? RowsShape{32, 29, 75, 1} : RowsShape{kFewRows, step, 45, 1};
   if (large) return {32, step + step / 2, 60, 1};
   // Tiles of 16 rows of narrow heads have 126 registers: four workgroups to a CU, whose steps take the longer.  us a call of one caller, D = 64, as two at 8 and 60 /
-  // as four at 15 and 45: 787+7218 behind 24, 32Q/8KV 71.1 / 51.5, 257+1643 behind 41, 64Q/8KV 33.0 / 25.5, 0+1032, 40Q/8KV 21.1 / 18.6, 4142+24 with 207+633, 16Q/4KV 12.8 / 12.7;
-  // 60 drawn batches 5 % less
+  // as four at 15 and 45: 787+7218 behind 24, 32Q/8KV 71.1 / 51.5, 257+1643 behind 41, 64Q/8KV 33.0 / 25.5, 0+1032, 40Q/8KV 21.1 / 18.6, 4142+24 with 207+633, 16Q/4KV 12.8 / 12.7
   if (head_dim <= 64) return {kFewRows, 15, 45, 1};
   return {kFewRows, step, head_dim < 128 ? 50 : 60, 1};
 }
