@@ -11,24 +11,22 @@ from window_harness import FULL
 
 pytestmark = pytest.mark.gpu
 
-SHAPES = [(8, 2, 128), (6, 2, 64), (4, 1, 256), (6, 3, 96), (8, 8, 48)]
+ROWS = [("5", "0", "1"), ("5", "0", "2"), ("5", "3", "1")]   # CALVO_ATTN_VARIANT: 5 the packed rows, 3 and 4 the pipelined kernels, of 128-wide heads alone
+PIPELINED = [("3", "0", "0"), ("4", "0", "0"), ("4", "3", "0")]
+CASES = [(*shape, *how) for shape in ((8, 2, 128), (6, 2, 64), (4, 1, 256), (6, 3, 96), (8, 8, 48)) for how in ROWS + PIPELINED * (shape[2] == 128)]
 
 
-def forced(monkeypatch, dim, variant, pieces, tile="0"):
-    """CALVO_ATTN_VARIANT: 3 and 4 the pipelined kernels, of 128-wide heads alone; 5 the packed rows."""
-    if variant != "5" and dim != 128:
-        pytest.skip("one kernel only")
+def forced(monkeypatch, variant, pieces, tile):
     monkeypatch.setenv("CALVO_ATTN_VARIANT", variant)
     monkeypatch.setenv("CALVO_ATTN_SPLITS", pieces)
     monkeypatch.setenv("CALVO_ROWS_TILE", tile)
 
 
-@pytest.mark.parametrize("hq,hkv,dim", SHAPES)
+@pytest.mark.parametrize("hq,hkv,dim,variant,pieces,tile", CASES)
 @pytest.mark.parametrize("byte", [0x7e, 0xf8])
-@pytest.mark.parametrize("variant,pieces,tile", [("3", "0", "0"), ("4", "0", "0"), ("4", "3", "0"), ("5", "0", "1"), ("5", "0", "2"), ("5", "3", "1")])
 def test_cached_values(hq, hkv, dim, byte, variant, pieces, tile, monkeypatch):
     """A block of V at scale 2^120 whose only byte that is not zero stands for +-448 or -256 times it, at one token and element."""
-    forced(monkeypatch, dim, variant, pieces, tile)
+    forced(monkeypatch, variant, pieces, tile)
     c = Case8([(150, 90)], hq, hkv, dim, seed=11)
     n8, t, window, n_first, poisoned = hkv * 16 * dim, c.tables[0], 40, 5, np.array([30, 120])
     for p in poisoned:
@@ -45,12 +43,11 @@ def test_cached_values(hq, hkv, dim, byte, variant, pieces, tile, monkeypatch):
     assert not torch.isfinite(out[..., 5]).any() and torch.isfinite(out[..., :5]).all() and torch.isfinite(out[..., 6:]).all()
 
 
-@pytest.mark.parametrize("hq,hkv,dim", SHAPES)
+@pytest.mark.parametrize("hq,hkv,dim,variant,pieces,tile", CASES)
 @pytest.mark.parametrize("value", [torch.finfo(torch.bfloat16).max, 1.9375 * 2.0 ** 127, -1.9375 * 2.0 ** 127])
-@pytest.mark.parametrize("variant,pieces,tile", [("3", "0", "0"), ("4", "0", "0"), ("5", "0", "1"), ("5", "0", "2"), ("5", "2", "1")])
 def test_appended_values(hq, hkv, dim, value, variant, pieces, tile, monkeypatch):
     """A chunk whose last token's V is finite in bf16 and rounds to 256 times the scale of 2^120: the last row alone is not finite there."""
-    forced(monkeypatch, dim, variant, pieces, tile)
+    forced(monkeypatch, variant, pieces, tile)
     c = Case8([(20, 30)], hq, hkv, dim, seed=12)
     c.v[0, -1, :, 7] = value
     got = c.run(FULL)
